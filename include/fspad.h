@@ -25,7 +25,9 @@
  *      output ("Partial Alignment Distillation": fspad_draft_layer), the top-k cut of
  *      a draft step's output and the
  *      choice of the tree from the candidates (Preliminaries, last paragraph:
- *      fspad_draft_topk, fspad_tree_build).
+ *      fspad_draft_topk, fspad_tree_build);
+ *   6. the same attention over a paged 4-bit cache, with the calls that keep it (fspad_tree_attn_paged,
+ *      fspad_page_map, fspad_kv_store_paged, fspad_kv_load_paged).
  *
  * Conventions that hold for every entry point:
  *   - "dev" pointers are device (HBM) addresses, "host" pointers are host
@@ -356,6 +358,142 @@ fspad_status fspad_kv_commit(const fspad_attn_desc* desc, const void* k_tree, co
                              void* k_cache, void* v_cache, int32_t cache_capacity,
                              const int32_t* kv_len, const int32_t* path, const int32_t* path_len,
                              int32_t* kv_len_out, void* hip_stream);
+
+/*
+ * Paged 4-bit cache (no passage of the paper: a storage format for serving long prompts, 17/64 of the bf16 cache's bytes).
+ * Four calls: fspad_page_map keeps block tables, slots and lengths on the device, fspad_kv_store_paged puts keys and values
+ * into pages, fspad_kv_load_paged takes them out, fspad_tree_attn_paged is the tree attention over them. Lengths and node
+ * counts are read from the DEVICE, so that a captured step replays with whatever the step before it accepted.
+ *
+ * Values. A block is 32 neighbouring channels of one token and kv head. An element is 4 bits, a sign on top of a code for 0,
+ * 1/2, 1, 3/2, 2, 3, 4, 6; a block's scale is 2^(s-127) for a byte s, and s = 255 makes all of the block NaN (the FP4 format of
+ * the OCP microscaling specification). The store rounds a block whose largest magnitude is a so:
+ *   s    = the smallest of 2..252 with a <= 7 * 2^(s-127)  (252 where that is too small too; 255 if any value is NaN or infinite)
+ *   code = the element nearest to x / 2^(s-127), ties to the even code, at most 6
+ * which is off by at most 2^(s-127) < a * 2/7 for a from 2^-123 to 7 * 2^125. What reads a cache takes s from 2 to 252, and 255;
+ * other scales are not specified.
+ *
+ * Pages. A page holds page_tokens tokens (16, 32, 64, 128 or 256) of all kv heads of one layer, one head after the other, of each
+ * (P = page_tokens, D = head_dim), in bytes:
+ *   K codes  [P][D/2]
+ *   V codes  [P*D/512][16][512/D][D/32]  groups of 512/D tokens; of a group, 16 runs of D/16 channels; of a run, token after token
+ *   K scales [D/32][P]
+ *   V scales [D/32][P]
+ * with the even channel of a byte in its low half: fspad_kv_page_bytes = Hkv * P * D * 17/16 in all. Pages start page_stride
+ * bytes apart (a multiple of 16, at least the page's bytes: pools of several layers may be interleaved) in a pool of n_pages;
+ * n_pages * page_tokens <= 2^31 - 1. Token t of page p is slot p * page_tokens + t.
+ */
+typedef struct {
+  int32_t batch;          /* B >= 1 (attention only, <= 1024) */
+  int32_t n_nodes_max;    /* Nmax, 1..64 (attention only) */
+  int32_t n_q_heads;      /* Hq (attention only) */
+  int32_t n_kv_heads;     /* Hkv, divides Hq */
+  int32_t head_dim;       /* D: 64 or 128 */
+  int32_t io_dtype;       /* FSPAD_BF16: q, k_tree, v_tree, and the rows that are stored and loaded */
+  int32_t out_dtype;      /* FSPAD_BF16 or FSPAD_F32 (attention only) */
+  float softmax_scale;    /* 0 => 1/sqrt(D); finite, of any sign, else 2^-125 at least in magnitude (attention only) */
+  int32_t page_tokens;    /* P: 16, 32, 64, 128 or 256 */
+  int32_t n_pages;        /* pages of the pool, >= 1 */
+  int64_t page_stride;    /* bytes from page to page */
+  int32_t table_width;    /* entries of a block table's row, >= 1 (attention only) */
+  int32_t max_kv_len;     /* no sequence is longer, 0..table_width * P (attention only): the launch is laid out for it */
+  int64_t table_stride;   /* entries from row to row of the block table, >= table_width (attention only) */
+  int32_t workgroups;     /* tuning of the attention: 0 = the built-in choice, 1..4096 forces the workgroup count; the
+                             workspace's size depends on it */
+  int32_t reserved;       /* 0 */
+} fspad_paged_desc;
+
+/* Bytes of one page, 0 for an unsupported shape. */
+size_t fspad_kv_page_bytes(int32_t n_kv_heads, int32_t head_dim, int32_t page_tokens);
+
+/*
+ * Page map: what a step changes of the block tables, in sequence order and by one rule on the device. Sequence b holds
+ * ceil(kv_len[b] / P) pages, the first entries of its row of the table. The stack free_pages[0 .. n_free-1] names the pages
+ * that nobody holds.
+ *   n_new[b] < 0   b ends: its pages go onto the stack (first those of the first sequence that ends, each row from its first
+ *                  entry on), kv_len_out[b] = 0, granted[b] = 0. Its row of the table keeps its entries.
+ *   n_new[b] >= 0  b grows by n_new[b] tokens. The pages it lacks for kv_len[b] + n_new[b] come off the top of the stack (which has
+ *                  the pages of the sequences that end by then), sequence after sequence, into its row: kv_len_out[b] = kv_len[b] +
+ *                  n_new[b], granted[b] = 1.
+ * A sequence is refused, kv_len_out[b] = kv_len[b] and granted[b] = 0 with its row as it was, if it would not fit its row, if
+ * n_new[b] > max_new or its rows would end past n_slots, or if it needs pages and those of all sequences up to it (refused for
+ * lack of pages or not, but not those refused for another reason) are more than the stack has.
+ *
+ * Slots of the new tokens (-1: none), for fspad_kv_store_paged:
+ *   max_new > 0, no path   slots [B,max_new]: token j < n_new[b] of a granted sequence has slots[b,j]
+ *   max_new > 0, path      slots [B,max_new] by tree node: place j < n_new[b] of the path has slots[b,path[b,j]] (path and path_len
+ *                          of an acceptance call as path and n_new, Nmax as max_new, at most 64; path entries outside [0,max_new) are
+ *                          not followed, of a node that is named twice the first place counts). The store then takes k_tree and v_tree as they are.
+ *   max_new = 0            slots [n_slots]: the sequences' rows one behind the other, max(n_new[b], 0) each whether granted or
+ *                          not; the rest of the array is -1. n_slots <= 2^22
+ *
+ *   B           1..2048;  table_width * P <= 2^31 - 1, B * table_width and B * max_new <= 2^30
+ *   kv_len, n_new, path    dev [B], [B], [B,max_new] i32 (negative lengths count as 0)
+ *   block_table dev [B] rows of table_width i32, table_stride entries apart: written where a sequence gets pages
+ *   free_pages  dev [n_pages] i32, in and out;  n_free dev [1] i32 (taken as 0..n_pages)
+ *   slots       dev out, may be NULL if it has no entries
+ *   kv_len_out, n_free_out, granted   dev [B], [1], [B] i32 out; kv_len_out may be kv_len and n_free_out n_free
+ * The pages of a sequence that ends must be its own, and no page may stand in two rows that end or on the stack twice. A table
+ * entry of a held page outside [0,n_pages) gives no slot. No workspace; allocates nothing, never synchronises.
+ */
+fspad_status fspad_page_map(int32_t B, int32_t page_tokens, int32_t n_pages, int32_t table_width, int64_t table_stride,
+                            const int32_t* kv_len, const int32_t* n_new, const int32_t* path, int32_t max_new,
+                            int32_t n_slots, int32_t* block_table, int32_t* free_pages, const int32_t* n_free,
+                            int32_t* slots, int32_t* kv_len_out, int32_t* n_free_out, int32_t* granted,
+                            void* hip_stream);
+
+/*
+ * Keys and values of `rows` tokens into the slots they are given, rounded as above (a prompt's tokens, or the tree's nodes with
+ * the slots that fspad_page_map made of the accepted path).
+ *   k, v      dev bf16, 16-byte aligned: channel c of head g of row r at r*row_stride + g*head_stride + c (elements, multiples
+ *             of 8, >= 0, the same for both)
+ *   slots     dev [rows] i32; a row whose slot is outside [0, n_pages * page_tokens) goes nowhere. No slot may be
+ *             given to two rows of a call (what it holds then is not specified)
+ *   pages     dev, 16-byte aligned; bytes of other slots stay as they are
+ * rows = 0 does nothing (no pointer is looked at). Reads n_kv_heads, head_dim, io_dtype, page_tokens, n_pages and page_stride of
+ * the descriptor, as fspad_kv_load_paged does.
+ */
+fspad_status fspad_kv_store_paged(const fspad_paged_desc* desc, int32_t rows, const void* k, const void* v,
+                                  int64_t row_stride, int64_t head_stride, const int32_t* slots,
+                                  void* pages, void* hip_stream);
+
+/*
+ * The reverse: row r of k and v (bf16, exact) is what slots[r] holds, zeros where the slot is outside [0, n_pages * page_tokens).
+ * Strides as for the store, both at least head_dim, and no two (row, head) pairs may share elements: the rows may be
+ * those of a cache that fspad_tree_attn reads. A slot may be given to several rows.
+ */
+fspad_status fspad_kv_load_paged(const fspad_paged_desc* desc, int32_t rows, const int32_t* slots, const void* pages,
+                                 void* k, void* v, int64_t row_stride, int64_t head_stride, void* hip_stream);
+
+/*
+ * Tree-masked attention over the pages: fspad_tree_attn with the prefix read through a block table from the 4-bit pool, and
+ * lengths and node counts from the device. One node (Nmax = 1, mask word 1) is plain decoding.
+ *
+ *   out[b,i,h,:] = sum_j softmax_j( scale * q[b,i,h,:] . K_j ) * V_j
+ * where j runs over the prefix positions t < kv_len[b] of kv head g = h/(Hq/Hkv) (slot
+ * block_table[b, t / P] * P + t % P) and then over the tree tokens t < n_nodes[b] whose bit t is set in anc_mask[b,i].
+ *
+ *   q, k_tree, v_tree   dev bf16 [B,Nmax,Hq,D], [B,Nmax,Hkv,D], 16-byte aligned, contiguous
+ *   pages       dev, 16-byte aligned
+ *   block_table dev [B] rows of table_width i32, table_stride entries apart. Positions on an entry outside [0,n_pages) are
+ *               left out, as if they were masked; entries past ceil(kv_len[b] / P) are not looked at
+ *   kv_len      DEV [B] i32, taken as 0 .. max_kv_len;  n_nodes DEV [B] i32, taken as 0 .. Nmax
+ *   anc_mask    dev [B,Nmax] u64 as for fspad_tree_attn
+ *   out         dev [B,Nmax,Hq,D] out_dtype, 16-byte aligned. Rows i >= n_nodes[b], and rows that see nothing, are zeros
+ *   workspace   dev, 16-byte aligned, >= fspad_tree_attn_paged_workspace_bytes(desc) (0: unsupported shape); contents ignored on entry,
+ *               undefined on exit; two calls that may overlap in time need different ones
+ * What a row does not see has no part in it, NaN and infinity included. Products are of bf16 values (the cached ones are
+ * exact in bf16, probabilities are rounded to bf16), sums fp32, the sum of the probabilities over the rounded ones. The same
+ * inputs give the same bits from run to run.
+ */
+size_t fspad_tree_attn_paged_workspace_bytes(const fspad_paged_desc* desc);
+
+fspad_status fspad_tree_attn_paged(const fspad_paged_desc* desc,
+                                   const void* q, const void* k_tree, const void* v_tree,
+                                   const void* pages, const int32_t* block_table,
+                                   const int32_t* kv_len, const int32_t* n_nodes,
+                                   const uint64_t* anc_mask, void* out,
+                                   void* workspace, size_t workspace_bytes, void* hip_stream);
 
 /*
  * Tile order for the weights of the skinny projections (an option of fspad_feature_sampler,

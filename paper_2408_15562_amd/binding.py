@@ -31,6 +31,8 @@ EXPORTS = ("fspad_tree_attn_workspace_bytes", "fspad_tree_attn",
            "fspad_tree_accept_sample_lm_head",
            "fspad_kv_commit", "fspad_feature_sampler_workspace_bytes", "fspad_feature_sampler",
            "fspad_draft_layer_workspace_bytes", "fspad_draft_layer", "fspad_packed_weight_bytes", "fspad_pack_weight",
+           "fspad_kv_page_bytes", "fspad_page_map", "fspad_kv_store_paged", "fspad_kv_load_paged",
+           "fspad_tree_attn_paged_workspace_bytes", "fspad_tree_attn_paged",
            "fspad_draft_topk_workspace_bytes", "fspad_draft_topk", "fspad_tree_build", "fspad_tree_build_mask",
            "fspad_tree_validate", "fspad_status_string")
 
@@ -48,6 +50,15 @@ class fspad_attn_desc(ctypes.Structure):
                 ("out_dtype", ctypes.c_int32), ("softmax_scale", ctypes.c_float),
                 ("cache_stride_batch", ctypes.c_int64), ("cache_stride_head", ctypes.c_int64),
                 ("cache_stride_token", ctypes.c_int64), ("workgroups", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
+class fspad_paged_desc(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("n_nodes_max", ctypes.c_int32), ("n_q_heads", ctypes.c_int32),
+                ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("io_dtype", ctypes.c_int32),
+                ("out_dtype", ctypes.c_int32), ("softmax_scale", ctypes.c_float), ("page_tokens", ctypes.c_int32),
+                ("n_pages", ctypes.c_int32), ("page_stride", ctypes.c_int64), ("table_width", ctypes.c_int32),
+                ("max_kv_len", ctypes.c_int32), ("table_stride", ctypes.c_int64), ("workgroups", ctypes.c_int32),
+                ("reserved", ctypes.c_int32)]
 
 
 class fspad_draft_layer_desc(ctypes.Structure):
@@ -115,6 +126,18 @@ def _lib():
         lib.fspad_draft_layer.restype = ctypes.c_int
         lib.fspad_draft_layer.argtypes = [ctypes.POINTER(fspad_draft_layer_desc),
                                           ctypes.POINTER(fspad_draft_layer_weights)] + [vp] * 11 + [vp, sz, vp]
+        lib.fspad_kv_page_bytes.restype = sz
+        lib.fspad_kv_page_bytes.argtypes = [i32, i32, i32]
+        lib.fspad_page_map.restype = ctypes.c_int
+        lib.fspad_page_map.argtypes = [i32, i32, i32, i32, i64, vp, vp, vp, i32, i32] + [vp] * 8
+        lib.fspad_kv_store_paged.restype = ctypes.c_int
+        lib.fspad_kv_store_paged.argtypes = [ctypes.POINTER(fspad_paged_desc), i32, vp, vp, i64, i64, vp, vp, vp]
+        lib.fspad_kv_load_paged.restype = ctypes.c_int
+        lib.fspad_kv_load_paged.argtypes = [ctypes.POINTER(fspad_paged_desc), i32, vp, vp, vp, vp, i64, i64, vp]
+        lib.fspad_tree_attn_paged_workspace_bytes.restype = sz
+        lib.fspad_tree_attn_paged_workspace_bytes.argtypes = [ctypes.POINTER(fspad_paged_desc)]
+        lib.fspad_tree_attn_paged.restype = ctypes.c_int
+        lib.fspad_tree_attn_paged.argtypes = [ctypes.POINTER(fspad_paged_desc)] + [vp] * 9 + [vp, sz, vp]
         lib.fspad_draft_topk_workspace_bytes.restype = sz
         lib.fspad_draft_topk_workspace_bytes.argtypes = [i32, i32, i32]
         lib.fspad_draft_topk.restype = ctypes.c_int
@@ -602,6 +625,179 @@ def fspad_draft_layer(eta: torch.Tensor, positions: torch.Tensor, weights: dict,
             _dev_ptr(workspace, "workspace"), workspace.numel() * workspace.element_size(), _stream_ptr(stream))
     keep = (desc, w, eta, positions, dict(weights), k_cache, v_cache, kv_len, n_nodes, anc_mask, outputs, workspace)
     return _issue(_lib().fspad_draft_layer, "fspad_draft_layer", args, keep, outputs, prepare)
+
+
+# ---- paged 4-bit cache (the format is in include/fspad.h)
+
+def fspad_kv_page_bytes(n_kv_heads: int, head_dim: int, page_tokens: int) -> int:
+    return int(_lib().fspad_kv_page_bytes(int(n_kv_heads), int(head_dim), int(page_tokens)))
+
+
+def _on_current_device(*tensors):
+    """The calls of the paged cache go to a stream of the current device: everything they touch has to be there."""
+    here = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.is_cuda and t.device.index != here:
+            raise ValueError("tensors must live on the current device")
+
+
+def _pool_desc(pages: torch.Tensor, head_dim: int) -> fspad_paged_desc:
+    """Geometry of a pool: uint8 [n_pages, Hkv, page_tokens * D * 17/16], a page's bytes without gaps, pages any stride apart."""
+    if pages.dtype != torch.uint8 or pages.dim() != 3:
+        raise ValueError("pages must be a uint8 [n_pages, n_kv_heads, bytes] device tensor")
+    n_pages, Hkv, per_head = pages.shape
+    if per_head and (pages.stride(2) != 1 or (Hkv > 1 and pages.stride(1) != per_head)):
+        raise ValueError("the bytes of a page must be contiguous")
+    if head_dim <= 0 or 16 * per_head % (17 * head_dim):
+        raise ValueError("pages must have page_tokens * head_dim * 17/16 bytes per kv head")
+    d = fspad_paged_desc()
+    d.batch = d.n_nodes_max = d.n_q_heads = d.table_width = d.table_stride = 1
+    d.n_kv_heads, d.head_dim, d.io_dtype, d.out_dtype = Hkv, int(head_dim), FSPAD_BF16, FSPAD_BF16
+    d.page_tokens, d.n_pages = 16 * per_head // (17 * head_dim), n_pages
+    d.page_stride = pages.stride(0) if n_pages > 1 else Hkv * per_head
+    return d
+
+
+def make_paged_desc(q: torch.Tensor, k_tree: torch.Tensor, pages: torch.Tensor, block_table: torch.Tensor,
+                    max_kv_len: Optional[int] = None, out_dtype: Optional[torch.dtype] = None, softmax_scale: float = 0.0,
+                    workgroups: int = 0) -> fspad_paged_desc:
+    """Fill the attention's descriptor from tensor shapes. max_kv_len: what the table's rows can hold, if not given."""
+    B, Nmax, Hq, D = q.shape
+    d = _pool_desc(pages, D)
+    if pages.shape[1] != k_tree.shape[2]:
+        raise ValueError("pages and k_tree must have the same kv heads")
+    if block_table.dtype != torch.int32 or block_table.dim() != 2 or block_table.shape[0] != B or block_table.stride(1) != 1:
+        raise ValueError("block_table must be an int32 [B, width] device tensor with contiguous rows")
+    d.batch, d.n_nodes_max, d.n_q_heads = B, Nmax, Hq
+    d.io_dtype = _dtype_code(q.dtype)
+    d.out_dtype = _dtype_code(out_dtype if out_dtype is not None else q.dtype)
+    d.softmax_scale, d.workgroups = float(softmax_scale), int(workgroups)
+    d.table_width = block_table.shape[1]
+    d.table_stride = block_table.stride(0) if B > 1 else block_table.shape[1]
+    d.max_kv_len = int(max_kv_len) if max_kv_len is not None else d.table_width * d.page_tokens
+    return d
+
+
+def fspad_tree_attn_paged_workspace_bytes(desc: fspad_paged_desc) -> int:
+    return int(_lib().fspad_tree_attn_paged_workspace_bytes(ctypes.byref(desc)))
+
+
+def fspad_tree_attn_paged(q: torch.Tensor, k_tree: torch.Tensor, v_tree: torch.Tensor, pages: torch.Tensor,
+                          block_table: torch.Tensor, kv_len: torch.Tensor, n_nodes: torch.Tensor, anc_mask: torch.Tensor,
+                          max_kv_len: Optional[int] = None, out: Optional[torch.Tensor] = None,
+                          workspace: Optional[torch.Tensor] = None, softmax_scale: float = 0.0,
+                          out_dtype: Optional[torch.dtype] = None, stream=None, desc: Optional[fspad_paged_desc] = None,
+                          prepare: bool = False, workgroups: int = 0):
+    """q [B,Nmax,Hq,D]; k_tree,v_tree [B,Nmax,Hkv,D]; pages uint8 [n_pages,Hkv,page bytes per head] (any page stride);
+    block_table int32 [B,width]; kv_len,n_nodes DEVICE int32 [B]; anc_mask device int64/uint64 [B,Nmax]. max_kv_len: no
+    sequence is longer (the launch is laid out for it). Returns out [B,Nmax,Hq,D]; with prepare=True a PreparedCall."""
+    B, Nmax, Hq, D = q.shape
+    for name, t, shape in (("q", q, tuple(q.shape)), ("k_tree", k_tree, (B, Nmax, k_tree.shape[2], D)),
+                           ("v_tree", v_tree, tuple(k_tree.shape))):
+        if not t.is_contiguous() or t.dtype != q.dtype or tuple(t.shape) != shape:
+            raise ValueError(f"{name} must be a contiguous {shape} tensor of q's dtype")
+    if desc is None:
+        desc = make_paged_desc(q, k_tree, pages, block_table, max_kv_len,
+                               out_dtype if out_dtype is not None else (out.dtype if out is not None else None), softmax_scale, workgroups)
+    for name, t in (("kv_len", kv_len), ("n_nodes", n_nodes)):
+        if t.dtype != torch.int32 or not t.is_contiguous() or tuple(t.shape) != (B,):
+            raise ValueError(f"{name} must be a contiguous int32 [B] device tensor")
+    if anc_mask.dtype not in (torch.int64, torch.uint64) or not anc_mask.is_contiguous() or tuple(anc_mask.shape) != (B, Nmax):
+        raise ValueError("anc_mask must be a contiguous 64-bit integer [B,Nmax] device tensor")
+    want = torch.float32 if desc.out_dtype == FSPAD_F32 else torch.bfloat16
+    if out is None:
+        out = torch.empty(q.shape, dtype=want, device=q.device)
+    if out.dtype != want or not out.is_contiguous() or out.shape != q.shape:
+        raise ValueError(f"out must be a contiguous {want} tensor of q's shape")
+    if workspace is None:
+        workspace = torch.empty(max(16, fspad_tree_attn_paged_workspace_bytes(desc)), dtype=torch.uint8, device=q.device)
+    args = (ctypes.byref(desc), _dev_ptr(q, "q"), _dev_ptr(k_tree, "k_tree"), _dev_ptr(v_tree, "v_tree"), _dev_ptr(pages, "pages"),
+            _dev_ptr(block_table, "block_table"), _dev_ptr(kv_len, "kv_len"), _dev_ptr(n_nodes, "n_nodes"),
+            _dev_ptr(anc_mask, "anc_mask"), _dev_ptr(out, "out"), _dev_ptr(workspace, "workspace"),
+            workspace.numel() * workspace.element_size(), _stream_ptr(stream))
+    _on_current_device(q, k_tree, v_tree, pages, block_table, kv_len, n_nodes, anc_mask, out, workspace)
+    keep = (desc, q, k_tree, v_tree, pages, block_table, kv_len, n_nodes, anc_mask, out, workspace)
+    return _issue(_lib().fspad_tree_attn_paged, "fspad_tree_attn_paged", args, keep, out, prepare)
+
+
+def _paged_rows(k, v, slots):
+    """Row and head strides that k and v [rows, Hkv, D] share."""
+    if k.dim() != 3 or v.shape != k.shape or v.dtype != torch.bfloat16 or k.dtype != torch.bfloat16:
+        raise ValueError("k and v must be bf16 [rows, n_kv_heads, head_dim] device tensors")
+    rows, Hkv, D = k.shape
+    if slots.dtype != torch.int32 or not slots.is_contiguous() or slots.numel() != rows:
+        raise ValueError("slots must be a contiguous int32 tensor with one entry per row")
+
+    def strides(t):   # (of an axis of one entry the stride says nothing)
+        return (t.stride(0) if rows > 1 else Hkv * D, t.stride(1) if Hkv > 1 else D)
+    if rows and (k.stride(2) != 1 or v.stride(2) != 1 or strides(k) != strides(v)):
+        raise ValueError("k and v must share their strides, with contiguous channels")
+    return rows, Hkv, D, (strides(k) if rows else (Hkv * D, D))
+
+
+def fspad_kv_store_paged(k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, pages: torch.Tensor, stream=None, prepare: bool = False):
+    """k,v bf16 [rows,Hkv,D] (rows and heads any stride apart, the same for both); slots int32, one per row (outside the pool: the
+    row goes nowhere); pages uint8 [n_pages,Hkv,page bytes per head]. With prepare=True a PreparedCall."""
+    rows, Hkv, D, (row_stride, head_stride) = _paged_rows(k, v, slots)
+    desc = _pool_desc(pages, D)
+    if pages.shape[1] != Hkv:
+        raise ValueError("pages must have the kv heads of k and v")
+    args = (ctypes.byref(desc), rows, _dev_ptr(k, "k"), _dev_ptr(v, "v"), row_stride, head_stride, _dev_ptr(slots, "slots"),
+            _dev_ptr(pages, "pages"), _stream_ptr(stream))
+    _on_current_device(k, v, slots, pages)
+    return _issue(_lib().fspad_kv_store_paged, "fspad_kv_store_paged", args, (desc, k, v, slots, pages), pages, prepare)
+
+
+def fspad_kv_load_paged(slots: torch.Tensor, pages: torch.Tensor, head_dim: int, outputs=None, stream=None, prepare: bool = False):
+    """Returns (k, v) bf16 [rows,Hkv,head_dim], rows = slots.numel(): what the slots hold, zeros for slots outside the pool. `outputs`
+    may bring the two tensors, with rows and heads any stride apart (a cache's own, say). With prepare=True a PreparedCall."""
+    desc = _pool_desc(pages, head_dim)
+    if outputs is None:
+        outputs = tuple(torch.empty((slots.numel(), pages.shape[1], head_dim), dtype=torch.bfloat16, device=pages.device) for _ in range(2))
+    k, v = outputs
+    rows, Hkv, D, (row_stride, head_stride) = _paged_rows(k, v, slots)
+    if Hkv != pages.shape[1] or D != head_dim:
+        raise ValueError("outputs must be [rows, kv heads of the pages, head_dim]")
+    args = (ctypes.byref(desc), rows, _dev_ptr(slots, "slots"), _dev_ptr(pages, "pages"), _dev_ptr(k, "k"), _dev_ptr(v, "v"), row_stride,
+            head_stride, _stream_ptr(stream))
+    _on_current_device(k, v, slots, pages)
+    return _issue(_lib().fspad_kv_load_paged, "fspad_kv_load_paged", args, (desc, slots, pages, k, v), (k, v), prepare)
+
+
+def fspad_page_map(kv_len: torch.Tensor, n_new: torch.Tensor, block_table: torch.Tensor, free_pages: torch.Tensor,
+                   n_free: torch.Tensor, page_tokens: int, path: Optional[torch.Tensor] = None, max_new: Optional[int] = None,
+                   n_slots: Optional[int] = None, outputs=None, stream=None, prepare: bool = False):
+    """Device int32 tensors: kv_len,n_new [B], block_table [B,width] (written), free_pages [n_pages] (the stack, written),
+    n_free [1], path [B,max_new] or None. Either max_new (slots [B,max_new]) or n_slots (packed slots [n_slots]). Returns (slots,
+    kv_len_out [B], n_free_out [1], granted [B]); `outputs` may bring them (kv_len and n_free themselves as the second and third:
+    updated in place). With prepare=True a PreparedCall."""
+    if (max_new is None) == (n_slots is None):
+        raise ValueError("give max_new or n_slots")
+    if max_new is not None and max_new < 1:
+        raise ValueError("max_new must be positive")
+    B = kv_len.numel()
+    shapes = [("kv_len", kv_len, (B,)), ("n_new", n_new, (B,)), ("free_pages", free_pages, (free_pages.numel(),)), ("n_free", n_free, (1,))]
+    if path is not None:
+        shapes.append(("path", path, (B, max_new)))
+    if block_table.dtype != torch.int32 or block_table.dim() != 2 or block_table.shape[0] != B or block_table.stride(1) != 1:
+        raise ValueError("block_table must be an int32 [B, width] device tensor with contiguous rows")
+    if outputs is None:
+        outputs = tuple(torch.empty(shape, dtype=torch.int32, device=kv_len.device)
+                        for shape in ((B, max_new) if max_new is not None else (n_slots,), (B,), (1,), (B,)))
+    slots, kv_len_out, n_free_out, granted = outputs
+    shapes += [("slots", slots, (B, max_new) if max_new is not None else (n_slots,)), ("kv_len_out", kv_len_out, (B,)),
+               ("n_free_out", n_free_out, (1,)), ("granted", granted, (B,))]
+    for name, t, shape in shapes:
+        if t.dtype != torch.int32 or not t.is_contiguous() or tuple(t.shape) != shape:
+            raise ValueError(f"{name} must be a contiguous int32 {shape} device tensor")
+    args = (B, int(page_tokens), free_pages.numel(), block_table.shape[1], block_table.stride(0) if B > 1 else block_table.shape[1],
+            _dev_ptr(kv_len, "kv_len"), _dev_ptr(n_new, "n_new"), _dev_ptr(path, "path"), int(max_new or 0), int(n_slots or 0),
+            _dev_ptr(block_table, "block_table"), _dev_ptr(free_pages, "free_pages"), _dev_ptr(n_free, "n_free"),
+            _dev_ptr(slots, "slots"), _dev_ptr(kv_len_out, "kv_len_out"), _dev_ptr(n_free_out, "n_free_out"),
+            _dev_ptr(granted, "granted"), _stream_ptr(stream))
+    _on_current_device(kv_len, n_new, path, block_table, free_pages, n_free, *outputs)
+    keep = (kv_len, n_new, path, block_table, free_pages, n_free)
+    return _issue(_lib().fspad_page_map, "fspad_page_map", args, keep, outputs, prepare)
 
 
 def fspad_draft_topk_workspace_bytes(rows: int, V: int, k: int) -> int:

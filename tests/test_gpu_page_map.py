@@ -1,0 +1,111 @@
+"""GPU page map against the oracle: whole numbers, equal in every entry, and what the call does not write left as it was."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2408_15562_amd as fspad
+from oracle import paged
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+def _dev(a):
+    return torch.from_numpy(np.ascontiguousarray(a, dtype=np.int32)).to(DEV)
+
+
+def _state(seed, B, P, len_max, width, spare):
+    """Lengths, a table of pages in random order (junk behind each row's pages) and the stack with junk above it."""
+    rng = np.random.default_rng(seed)
+    kv_len = rng.integers(0, min(len_max, width * P) + 1, B)
+    held = -(-kv_len // P)
+    order = rng.permutation(max(1, int(held.sum()) + spare))   # (a pool has a page at least)
+    table = rng.integers(-5, 10 ** 6, (B, width))
+    at = 0
+    for b in range(B):
+        table[b, :held[b]] = order[at:at + held[b]]
+        at += held[b]
+    free = rng.integers(-9, 10 ** 6, len(order))
+    free[:len(order) - at] = order[at:]
+    return rng, kv_len, table, free
+
+
+def _check(kv_len, n_new, table, free, n_free, P, path=None, max_new=None, n_slots=None, in_place=False, pad=3):
+    B, width = table.shape
+    wide = np.full((B, width + pad), -77)
+    wide[:, :width] = table
+    t, f = _dev(wide), _dev(free)
+    lens, top = _dev(kv_len), _dev([n_free])
+    outputs = None
+    if in_place:
+        shape = (B, max_new) if max_new is not None else (n_slots,)
+        outputs = (torch.full(shape, -99, dtype=torch.int32, device=DEV), lens, top, torch.full((B,), -99, dtype=torch.int32, device=DEV))
+    got = fspad.fspad_page_map(lens, _dev(n_new), t[:, :width], f, top, P, path=None if path is None else _dev(path), max_new=max_new,
+                               n_slots=n_slots, outputs=outputs)
+    torch.cuda.synchronize()
+    want = paged.page_map(kv_len, n_new, table, free, [n_free], P, path=path, max_new=max_new, n_slots=n_slots)
+    for name, g, w in zip(("slots", "kv_len_out", "n_free_out", "granted", "table", "free"), (*got, t[:, :width], f), want):
+        assert np.array_equal(g.cpu().numpy(), w), name
+    assert bool((t[:, width:] == -77).all())
+    return want
+
+
+@pytest.mark.parametrize("B,P,len_max,new_max", [(1, 16, 0, 1), (1, 64, 5000, 300), (3, 16, 100, 40), (16, 32, 6000, 7), (65, 16, 700, 33), (257, 64, 900, 70),
+                                                 (300, 128, 3000, 1200), (2048, 256, 2000, 5)])
+@pytest.mark.parametrize("form", ["rows", "path", "packed"])
+@pytest.mark.parametrize("spare", ["plenty", "short", "none"])
+def test_map_matches_oracle(B, P, len_max, new_max, form, spare):
+    if form == "path":
+        new_max = min(new_max, 64)
+    width = -(-(len_max + new_max) // P) + 1
+    n_spare = {"plenty": B * (new_max // P + 2), "short": max(1, B * new_max // P // 2), "none": 0}[spare]
+    rng, kv_len, table, free = _state(B + P, B, P, len_max, width, n_spare)
+    n_new = rng.integers(0, new_max + 1, B)
+    if B > 2:
+        n_new[rng.random(B) < 0.2] = -1
+        n_new[rng.integers(B)] = 0
+    path = None
+    if form == "path":
+        path = np.stack([rng.permutation(64)[:new_max] for _ in range(B)]) if new_max > 8 else rng.integers(-2, new_max + 2, (B, new_max))
+    kw = dict(n_slots=int(np.maximum(n_new, 0).sum()) + 3) if form == "packed" else dict(max_new=new_max)
+    for in_place in (False, True):
+        _check(kv_len, n_new, table, free, n_spare, P, path=path, in_place=in_place, **kw)
+
+
+def test_refusals_are_of_one_sequence_alone():
+    """A row that is full, more tokens than rows, a packed array that ends, a length that no table holds: the others go on."""
+    P, width = 16, 4
+    table = np.arange(24).reshape(6, 4)
+    free = np.arange(24, 64)
+    kv_len = np.array([60, 64, 5, 2 ** 31 - 1, 0, 33])
+    n_new = np.array([5, 1, 9, 0, 0, -3])
+    want = _check(kv_len, n_new, table, free, 40, P, max_new=8)
+    assert list(want[3]) == [0, 0, 0, 0, 1, 0]
+    want = _check(kv_len, np.array([4, 0, 9, 1, 2, 31]), table, free, 40, P, n_slots=16)
+    assert list(want[3]) == [1, 1, 1, 0, 1, 0]
+    want = _check(np.array([-5, 3, 4, 5, 6, 7]), np.array([2 ** 31 - 1, 2 ** 31 - 1, 2, 2 ** 31 - 1, 1, 0]), table, free, 40, P, n_slots=50)
+    assert list(want[3]) == [0, 0, 0, 0, 0, 0]
+    _check(np.array([-5, 3, 4, 5, 6, 7]), np.array([2 ** 31 - 1, 2 ** 31 - 1, 2, 1, -2 ** 31, 0]), table, free, 40, P, max_new=3)
+
+
+def test_pages_that_come_back_are_handed_out_in_the_same_call():
+    P = 32
+    table = np.array([[7, 3, 1, -1], [5, -1, -1, -1], [0, 2, -1, -1]])
+    free = np.array([4, -1, -1, -1, -1, -1, -1, -1])
+    want = _check(np.array([96, 20, 40]), np.array([-1, 100, 30]), table, free, 1, P, max_new=100)
+    assert list(want[3]) == [0, 1, 1] and list(want[4][1]) == [5, 1, 3, 7] and list(want[4][2]) == [0, 2, 4, -1] and int(want[2][0]) == 0
+
+
+@pytest.mark.parametrize("n_free", [-4, 100])
+def test_a_stack_height_outside_the_stack(n_free):
+    table = np.array([[1, 0], [2, -1]])
+    free = np.array([3, 4, 5, 6])
+    _check(np.array([20, 4]), np.array([1, 20]), table, free, n_free, 16, max_new=20)
+    _check(np.array([20, 4]), np.array([-1, 20]), table, free, n_free, 16, max_new=20)
+
+
+def test_bad_table_entries_give_no_slots():
+    table = np.array([[9, 50, -1], [-3, 1, -1]])
+    free = np.array([3, 4, 77, 5] + [6] * 8)
+    want = _check(np.array([20, 4]), np.array([4, 30]), table, free, 3, 16, max_new=30)
+    assert np.all(want[0][0] == -1) and np.all(want[0][1, :12] == -1) and want[0][1, 12] == -1 and list(want[3]) == [1, 1]

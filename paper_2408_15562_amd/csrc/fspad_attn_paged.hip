@@ -23,6 +23,7 @@
 #include "fspad.h"
 #include "paged_layout.h"
 #include "paged_plan.h"
+#include "wave_scan.h"
 
 namespace {
 
@@ -89,16 +90,9 @@ __device__ __forceinline__ SeqChunk load_chunk(const PagedParams& p, int chunk, 
   const int b = 64 * chunk + lane;
   c.s = shape_of(p, b < p.B ? p.kv_len[b] : 0, b < p.B ? p.n_nodes[b] : 0);
   if (b >= p.B) c.s.flat = 0;
-  unsigned sum = c.s.flat;
-  if (p.B > 1) {
-#pragma unroll
-    for (int off = 1; off < 64; off <<= 1) {
-      const unsigned y = __shfl_up(sum, off);
-      if (lane >= off) sum += y;
-    }
-  }
+  const unsigned sum = (unsigned)wave_sum_upto((int)c.s.flat);
   c.first = begin + sum - c.s.flat;
-  c.end = begin + (p.B > 1 ? __builtin_amdgcn_readlane(sum, 63) : __builtin_amdgcn_readlane(sum, 0));
+  c.end = begin + (unsigned)__builtin_amdgcn_readlane((int)sum, 63);
   return c;
 }
 

@@ -6,6 +6,7 @@
 
 #include "fspad.h"
 #include "paged_layout.h"
+#include "wave_scan.h"
 
 namespace {
 
@@ -194,39 +195,35 @@ struct MapParams {
   int32_t B, page_shift, n_pages, width, max_new, n_slots;   // max_new = 0: packed slots
 };
 
-constexpr int kMapThreads = 256, kMapWaves = kMapThreads / 64;
 constexpr int kMapMaxBatch = 2048;
 constexpr int kMapMaxPacked = 1 << 22;
 constexpr int64_t kMapMaxEntries = 1 << 30;   // of a list: indexes and one step of the grid past them stay 32-bit
+// Entries (slots, and a quarter of the tables', for the pages that a call moves) that one workgroup does alone; a workgroup's share of
+// more: an item a thread; workgroups at most.
+constexpr int64_t kMapAlone = 4096, kMapShare = 1024, kMapMostWgs = 1024;
 enum : int { kGranted = 1, kEnded = 2 };
 
+// What a workgroup knows of every sequence (dynamic LDS, seven arrays of B words).
 struct MapShared {
-  int len[kMapMaxBatch];          // lengths before the call
-  int add[kMapMaxBatch];          // tokens asked for
-  int have[kMapMaxBatch];         // pages held before the call
-  int need_before[kMapMaxBatch];  // pages needed by the sequences before this one
-  int back_before[kMapMaxBatch];  // pages that the ended sequences before this one give back
-  int row_before[kMapMaxBatch];   // packed rows of the sequences before this one
-  unsigned char flags[kMapMaxBatch];
-  int wave_sum[3][kMapWaves];
-  int taken[kMapWaves];
+  int *len, *add, *have;  // length before the call, tokens asked for, pages held before the call
+  int* need_before;       // pages needed by the sequences before this one
+  int* back_before;       // pages that the ended sequences before this one give back
+  int* row_before;        // packed rows of the sequences before this one
+  int* flags;
 };
+constexpr int kMapArrays = 7;
 
 // Sum of x over the threads before this one; over all of them in `all`.
+template <int THREADS>
 __device__ __forceinline__ int sum_before(int x, int* wave_sum, int& all) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  int s = x;
-#pragma unroll
-  for (int off = 1; off < 64; off <<= 1) {
-    const int y = __shfl_up(s, off);
-    if (lane >= off) s += y;
-  }
+  const int s = wave_sum_upto(x);
   if (lane == 63) wave_sum[wave] = s;
   __syncthreads();
   int before = 0;
   all = 0;
 #pragma unroll
-  for (int w = 0; w < kMapWaves; ++w) {
+  for (int w = 0; w < THREADS / 64; ++w) {
     if (w < wave) before += wave_sum[w];
     all += wave_sum[w];
   }
@@ -243,11 +240,13 @@ __device__ __forceinline__ int owner_in(const int* before, int B, int x) {
   return lo;
 }
 
-template <bool LISTS, bool LENGTHS>
-__global__ __launch_bounds__(kMapThreads) void page_map_kernel(const MapParams p) {
-  __shared__ MapShared sh;
+template <bool LISTS, bool LENGTHS, int THREADS>
+__global__ __launch_bounds__(THREADS) void page_map_kernel(const MapParams p) {
+  extern __shared__ int arrays[];
+  __shared__ int wave_sum[3][THREADS / 64], wave_taken[THREADS / 64];
+  const MapShared sh = {arrays, arrays + p.B, arrays + 2 * p.B, arrays + 3 * p.B, arrays + 4 * p.B, arrays + 5 * p.B, arrays + 6 * p.B};
   const int tid = threadIdx.x, P = 1 << p.page_shift;
-  const int per = (p.B + kMapThreads - 1) / kMapThreads;   // a thread has a run of neighbouring sequences
+  const int per = (p.B + THREADS - 1) / THREADS;   // a thread has a run of neighbouring sequences
   const int b0 = tid * per, b1 = min(b0 + per, p.B);
   const int n_free = min(max(*p.n_free, 0), p.n_pages);
   const int64_t room = (int64_t)p.width << p.page_shift;
@@ -264,8 +263,8 @@ __global__ __launch_bounds__(kMapThreads) void page_map_kernel(const MapParams p
   }
   // (rows past the end of a packed array: a share of more than the array holds counts as one more than that)
   int back_all, row_all, need_all;
-  int back_at = sum_before(back_sum, sh.wave_sum[0], back_all);
-  int64_t row_at = sum_before(p.max_new > 0 ? 0 : (int)min(row_sum, (int64_t)p.n_slots + 1), sh.wave_sum[1], row_all);
+  int back_at = sum_before<THREADS>(back_sum, wave_sum[0], back_all);
+  int64_t row_at = sum_before<THREADS>(p.max_new > 0 ? 0 : (int)min(row_sum, (int64_t)p.n_slots + 1), wave_sum[1], row_all);
   const int avail = min(n_free + back_all, p.n_pages);
   int need_sum = 0;
   for (int b = b0; b < b1; ++b) {
@@ -273,7 +272,7 @@ __global__ __launch_bounds__(kMapThreads) void page_map_kernel(const MapParams p
     const bool ended = add < 0;
     const bool fits = !ended && (int64_t)len + add <= room && (p.max_new > 0 ? add <= p.max_new : row_at + add <= p.n_slots);
     const int need = fits ? (int)(((int64_t)len + add + P - 1) >> p.page_shift) - have : 0;
-    sh.flags[b] = (unsigned char)(ended ? kEnded : fits ? kGranted : 0);
+    sh.flags[b] = (ended ? kEnded : fits ? kGranted : 0);
     sh.back_before[b] = back_at;
     sh.row_before[b] = (int)min(row_at, (int64_t)p.n_slots + 1);
     sh.need_before[b] = need;
@@ -281,7 +280,7 @@ __global__ __launch_bounds__(kMapThreads) void page_map_kernel(const MapParams p
     back_at += ended ? have : 0;
     row_at += max(add, 0);
   }
-  int need_at = sum_before(need_sum, sh.wave_sum[2], need_all);
+  int need_at = sum_before<THREADS>(need_sum, wave_sum[2], need_all);
   int taken = 0;
   for (int b = b0; b < b1; ++b) {
     const int need = sh.need_before[b];
@@ -295,26 +294,64 @@ __global__ __launch_bounds__(kMapThreads) void page_map_kernel(const MapParams p
   __syncthreads();
 
   if constexpr (LISTS) {
-    const int at = blockIdx.x * kMapThreads + tid, step = gridDim.x * kMapThreads;
+    const int at = blockIdx.x * THREADS + tid, step = gridDim.x * THREADS;
     // entry x of the stack as the pushes leave it
     auto stacked = [&](int x) {
       if (x < n_free) return p.free_pages[x];
       const int b = owner_in(sh.back_before, p.B, x - n_free);
       return p.table[b * p.table_stride + (x - n_free - sh.back_before[b])];
     };
-    for (int x = at; x < back_all; x += step)
-      if (n_free + x < p.n_pages) p.free_pages[n_free + x] = stacked(n_free + x);
-    for (int x = at; x < min(need_all, avail); x += step) {
-      const int b = owner_in(sh.need_before, p.B, x);
-      if (sh.flags[b] == kGranted) p.table[b * p.table_stride + sh.have[b] + (x - sh.need_before[b])] = stacked(avail - 1 - x);
-    }
     // slot of token j of sequence b: in a page it has, or in one that it gets
-    auto slot_of = [&](int b, int j) {
-      const int pos = sh.len[b] + j, i = pos >> p.page_shift, fresh = i - sh.have[b];
-      const int page = fresh < 0 ? p.table[b * p.table_stride + i] : stacked(avail - 1 - (sh.need_before[b] + fresh));
-      // (an entry that names no page: no slot)
+    auto page_of = [&](int b, int i) {
+      const int fresh = i - sh.have[b];
+      return fresh < 0 ? p.table[b * p.table_stride + i] : stacked(avail - 1 - (sh.need_before[b] + fresh));
+    };
+    auto slot_in = [&](int page, int pos) {   // (an entry that names no page: no slot)
       return (unsigned)page < (unsigned)p.n_pages ? (page << p.page_shift) + (pos & (P - 1)) : -1;
     };
+    // One list of everything that is written, so that the threads share it evenly whatever it is made of: pushes, entries of the
+    // tables, slots four at a time
+    const int pushes = back_all, entries = min(need_all, avail), total = p.max_new > 0 ? p.B * p.max_new : p.n_slots;
+    const int64_t items = (int64_t)pushes + entries + (p.path ? 0 : (total + 3) / 4);
+    for (int64_t item = at; item < items; item += step) {
+      if (item < pushes) {
+        const int x = n_free + (int)item;
+        if (x < p.n_pages) p.free_pages[x] = stacked(x);
+        continue;
+      }
+      if (item < pushes + entries) {
+        const int x = (int)item - pushes, b = owner_in(sh.need_before, p.B, x);
+        if (sh.flags[b] == kGranted) p.table[b * p.table_stride + sh.have[b] + (x - sh.need_before[b])] = stacked(avail - 1 - x);
+        continue;
+      }
+      const int x0 = 4 * (int)(item - pushes - entries);
+      int b = p.max_new > 0 ? x0 / p.max_new : owner_in(sh.row_before, p.B, x0), known = -1, page = -1;
+      int slot[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int x = x0 + k;
+        int first = p.max_new > 0 ? b * p.max_new : sh.row_before[b];
+        // (the next sequence that has this entry; the last one has all that are left)
+        while (b + 1 < p.B) {
+          const int next = p.max_new > 0 ? first + p.max_new : sh.row_before[b + 1];
+          if (x < next) break;
+          ++b;
+          first = next;
+          known = -1;
+        }
+        const int j = x - first;
+        slot[k] = -1;
+        if (x < total && sh.flags[b] == kGranted && j < sh.add[b]) {
+          const int pos = sh.len[b] + j, i = pos >> p.page_shift;
+          if (i != known) page = page_of(b, i);
+          known = i;
+          slot[k] = slot_in(page, pos);
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (x0 + k < total) p.slots[x0 + k] = slot[k];
+    }
     if (p.path) {   // a wavefront a sequence: lane i is node i of the tree, and lane j held place j of its path
       const int lane = tid & 63;
       for (int b = at >> 6; b < p.B; b += step >> 6) {
@@ -323,23 +360,19 @@ __global__ __launch_bounds__(kMapThreads) void page_map_kernel(const MapParams p
         int place = -1;
         for (int j = add - 1; j >= 0; --j)   // (a node that is named twice has its first place)
           if (__shfl(node, j) == lane) place = j;
-        if (lane < p.max_new) p.slots[(int64_t)b * p.max_new + lane] = place >= 0 ? slot_of(b, place) : -1;
-      }
-    } else {
-      const int total = p.max_new > 0 ? p.B * p.max_new : p.n_slots;
-      for (int x = at; x < total; x += step) {
-        const int b = p.max_new > 0 ? x / p.max_new : owner_in(sh.row_before, p.B, x);
-        const int j = p.max_new > 0 ? x - b * p.max_new : x - sh.row_before[b];
-        p.slots[x] = sh.flags[b] == kGranted && j < sh.add[b] ? slot_of(b, j) : -1;
+        if (lane < p.max_new) {
+          const int pos = sh.len[b] + place;
+          p.slots[(int64_t)b * p.max_new + lane] = place >= 0 ? slot_in(page_of(b, pos >> p.page_shift), pos) : -1;
+        }
       }
     }
   }
-  if constexpr (LENGTHS) {
+  if (LENGTHS && blockIdx.x == 0) {
 #pragma unroll
     for (int off = 32; off > 0; off >>= 1) taken = max(taken, __shfl_xor(taken, off));
-    if ((tid & 63) == 0) sh.taken[tid >> 6] = taken;
+    if ((tid & 63) == 0) wave_taken[tid >> 6] = taken;
     __syncthreads();
-    for (int b = tid; b < p.B; b += kMapThreads) {
+    for (int b = tid; b < p.B; b += THREADS) {
       const int f = sh.flags[b];
       p.kv_len_out[b] = f == kEnded ? 0 : sh.len[b] + (f == kGranted ? sh.add[b] : 0);
       p.granted[b] = f == kGranted;
@@ -347,7 +380,7 @@ __global__ __launch_bounds__(kMapThreads) void page_map_kernel(const MapParams p
     if (tid == 0) {
       int most = 0;
 #pragma unroll
-      for (int w = 0; w < kMapWaves; ++w) most = max(most, sh.taken[w]);
+      for (int w = 0; w < THREADS / 64; ++w) most = max(most, wave_taken[w]);
       *p.n_free_out = avail - most;
     }
   }
@@ -391,6 +424,22 @@ extern "C" fspad_status fspad_page_map(int32_t B, int32_t page_tokens, int32_t n
   p.B = B; p.page_shift = log2_of(page_tokens); p.n_pages = n_pages; p.width = table_width;
   p.max_new = max_new; p.n_slots = max_new > 0 ? 0 : n_slots;
   hipStream_t stream = reinterpret_cast<hipStream_t>(hip_stream);
-  hipLaunchKernelGGL((page_map_kernel<true, true>), dim3(1), dim3(kMapThreads), 0, stream, p);
+  const int64_t entries = max_new > 0 ? (int64_t)B * max_new : n_slots;
+  const int64_t work = entries + (int64_t)B * table_width / 4;
+  const unsigned lds = (unsigned)(kMapArrays * B * sizeof(int));
+  if (work <= kMapAlone) {
+    hipLaunchKernelGGL((page_map_kernel<true, true, 1024>), dim3(1), dim3(1024), lds, stream, p);
+  } else {
+    // lengths or the stack's height in place: behind the workgroups that read them
+    const bool in_place = (kv_len_out < kv_len + B && kv_len < kv_len_out + B) || n_free_out == n_free;
+    int64_t wgs = (work + kMapShare - 1) / kMapShare;
+    if (wgs > kMapMostWgs) wgs = kMapMostWgs;
+    if (in_place) {
+      hipLaunchKernelGGL((page_map_kernel<true, false, 256>), dim3((unsigned)wgs), dim3(256), lds, stream, p);
+      hipLaunchKernelGGL((page_map_kernel<false, true, 256>), dim3(1), dim3(256), lds, stream, p);
+    } else {
+      hipLaunchKernelGGL((page_map_kernel<true, true, 256>), dim3((unsigned)wgs), dim3(256), lds, stream, p);
+    }
+  }
   return hipGetLastError() == hipSuccess ? FSPAD_OK : FSPAD_ERR_HIP;
 }

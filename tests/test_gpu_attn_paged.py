@@ -80,8 +80,9 @@ class Case:
 def _compare(got, want, bound):
     assert np.array_equal(np.isfinite(got), np.isfinite(want))
     f = np.isfinite(want)
-    over = np.abs(got - want)[f] - bound[f]
-    assert over.size == 0 or over.max() <= 0.0, f"off by {np.abs(got - want)[f].max():.3g}, {over.max():.3g} more than the bound allows"
+    off = np.abs(got[f] - want[f])
+    over = off - bound[f]
+    assert over.size == 0 or over.max() <= 0.0, f"off by {off.max():.3g}, {over.max():.3g} more than the bound allows"
 
 
 @pytest.mark.parametrize("D,P", [(64, 16), (128, 16), (128, 32), (64, 64), (128, 64), (128, 256), (64, 256)])

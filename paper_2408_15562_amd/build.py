@@ -26,7 +26,7 @@ _FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
 # per-source options. The attention kernels keep the results of their matrix instructions in ordinary
 # vector registers: left to itself the compiler puts the score tiles into accumulation registers and
 # copies every one of them out again for the softmax (a quarter of the instructions of a block).
-EXTRA_FLAGS = {"fspad_attn.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
+EXTRA_FLAGS = {src: ["-mllvm", "-amdgpu-mfma-vgpr-form=1"] for src in ("fspad_attn.hip", "fspad_attn_paged.hip")}
 
 
 def compile_command(src: str, obj: str, defines=()):

@@ -140,35 +140,37 @@ __device__ __forceinline__ unsigned two_values(unsigned codes, float scale, int 
                                                                                            : two_values<3>(codes, scale);
 }
 
-// A 32-key block of the prefix as it lies in the pages. Keys that are not there (past the length, on a bad page) are masked by their
-// scores; their values only have to be finite, which codes are under any scale but 255.
+// K and V of a 32-key block of the prefix as they lie in the pages. Keys that are not there (past the length, on a bad page) are
+// masked by their scores; their values only have to be finite, which codes are under any scale but 255.
 template <int D>
-struct PagedBlock {
-  unsigned k[2][D / 32], k_scale[2];
-  unsigned v[D / 16];
-  u32x2 v_scale;
-  unsigned vis;        // bit t: key t is there
-  float sv[8];
+struct PagedK {
+  unsigned c[2][D / 32], scale[2];
 
-  __device__ __forceinline__ void ready(int g4) {
+  __device__ __forceinline__ bf16x8 k_frag(int kt, int ks) const {
+    const float f = __builtin_bit_cast(float, scale[kt] << 23);
+    const unsigned w = c[kt][ks];
+    const u32x4 x = {two_values<0>(w, f), two_values<1>(w, f), two_values<2>(w, f), two_values<3>(w, f)};
+    return __builtin_bit_cast(bf16x8, x);
+  }
+};
+template <int D>
+struct PagedV {
+  unsigned c[D / 16];
+  unsigned scale[2];
+  float f[8];   // scales of the lane's keys
+
+  __device__ __forceinline__ void ready(unsigned vis, int g4) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) sv[j] = __builtin_bit_cast(float, ((v_scale[j >> 2] >> (8 * (j & 3))) & 0xffu) << 23);
+    for (int j = 0; j < 8; ++j) f[j] = __builtin_bit_cast(float, ((scale[j >> 2] >> (8 * (j & 3))) & 0xffu) << 23);
     if (vis != ~0u) {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) sv[j] = ((vis >> (8 * g4 + j)) & 1u) ? sv[j] : 1.0f;
+      for (int j = 0; j < 8; ++j) f[j] = ((vis >> (8 * g4 + j)) & 1u) ? f[j] : 1.0f;
     }
-  }
-  __device__ __forceinline__ bf16x8 k_frag(int kt, int ks) const {
-    const float scale = __builtin_bit_cast(float, k_scale[kt] << 23);
-    const unsigned c = k[kt][ks];
-    const u32x4 x = {two_values<0>(c, scale), two_values<1>(c, scale), two_values<2>(c, scale), two_values<3>(c, scale)};
-    return __builtin_bit_cast(bf16x8, x);
   }
   __device__ __forceinline__ void v_pair(int e2, bf16x8& even, bf16x8& odd) const {
     unsigned x[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j)
-      x[j] = D == 128 ? two_values(v[j], sv[j], e2) : two_values(v[j >> 1], sv[j], 2 * (j & 1) + e2);
+    for (int j = 0; j < 8; ++j) x[j] = D == 128 ? two_values(c[j], f[j], e2) : two_values(c[j >> 1], f[j], 2 * (j & 1) + e2);
     turn(x, even, odd);
   }
 };
@@ -192,32 +194,38 @@ __device__ __forceinline__ unsigned wild_halves(unsigned w) {   // all bits of a
   return ((w & 0x7f80u) == 0x7f80u ? 0xffffu : 0u) | ((w & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u);
 }
 
-// One block against the wavefront's rows. visible(t): the 32 keys that this lane's row of tile t sees; full: all of them for every row.
-template <int QT, int D, typename Block, typename VisibleFn>
-__device__ __forceinline__ void process_block(RowState<QT, D>& st, const Block& blk, const bf16x8 (&qf)[QT][D / 32], bool full,
-                                              VisibleFn&& visible, float c, int g4, bf16x8 (&pf)[QT]) {
-  constexpr int DT = D / 16, KS = D / 32;
-  f32x4 s[QT][2];
+template <int QT>
+using Scores = f32x4[QT][2];   // lane (col, g4), [t][kt][i]: key 8 g4 + 4 kt + i against row 16 t + col
+
+template <int QT, int D, typename Keys>
+__device__ __forceinline__ void score_block(Scores<QT>& s, const Keys& keys, const bf16x8 (&qf)[QT][D / 32]) {
 #pragma unroll
   for (int t = 0; t < QT; ++t) s[t][0] = s[t][1] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
   for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks) {
-      const bf16x8 a = blk.k_frag(kt, ks);
+    for (int ks = 0; ks < D / 32; ++ks) {
+      const bf16x8 a = keys.k_frag(kt, ks);
 #pragma unroll
       for (int t = 0; t < QT; ++t) s[t][kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, qf[t][ks], s[t][kt], 0, 0, 0);
     }
-  if (!full) {   // wavefront-uniform
-    const float hidden = c < 0.f ? INFINITY : -INFINITY;   // (times c: below every score)
+}
+
+// Hides what a row does not see; visible(t): the 32 keys that this lane's row of tile t does.
+template <int QT, typename VisibleFn>
+__device__ __forceinline__ void hide(Scores<QT>& s, VisibleFn&& visible, float c, int g4) {
+  const float hidden = c < 0.f ? INFINITY : -INFINITY;   // (times c: below every score)
 #pragma unroll
-    for (int t = 0; t < QT; ++t) {
-      const unsigned vis = visible(t) >> (8 * g4);
+  for (int t = 0; t < QT; ++t) {
+    const unsigned vis = visible(t) >> (8 * g4);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) s[t][j >> 2][j & 3] = ((vis >> j) & 1u) ? s[t][j >> 2][j & 3] : hidden;
-    }
+    for (int j = 0; j < 8; ++j) s[t][j >> 2][j & 3] = ((vis >> j) & 1u) ? s[t][j >> 2][j & 3] : hidden;
   }
-  float x[QT][8];   // exponents of the weights under the shift in use
+}
+
+// Exponents of the weights, under the shifts in use or, where a score is too far above its row's, under shifts that move.
+template <int QT, int D>
+__device__ __forceinline__ void exponents(RowState<QT, D>& st, const Scores<QT>& s, float (&x)[QT][8], float c) {
   bool grow = false;
 #pragma unroll
   for (int t = 0; t < QT; ++t) {
@@ -240,12 +248,16 @@ __device__ __forceinline__ void process_block(RowState<QT, D>& st, const Block& 
       st.m[t] = moved;
       st.l[t] *= alpha;
 #pragma unroll
-      for (int e = 0; e < DT; ++e) st.o[t][e] *= alpha;
+      for (int e = 0; e < D / 16; ++e) st.o[t][e] *= alpha;
 #pragma unroll
       for (int j = 0; j < 8; ++j) x[t][j] = fmaf(s[t][j >> 2][j & 3], c, -moved);
     }
   }
-  // weights are rounded to bf16, which is what the matrix cores take; their sum is that of the rounded ones
+}
+
+// Weights are rounded to bf16, which is what the matrix cores take; their sum is that of the rounded ones.
+template <int QT, int D, typename Values>
+__device__ __forceinline__ void accumulate(RowState<QT, D>& st, const float (&x)[QT][8], const Values& values, bf16x8 (&pf)[QT]) {
 #pragma unroll
   for (int t = 0; t < QT; ++t)
 #pragma unroll
@@ -256,9 +268,9 @@ __device__ __forceinline__ void process_block(RowState<QT, D>& st, const Block& 
 #pragma unroll
   for (int t = 0; t < QT; ++t) st.l[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pf[t], st.l[t], 0, 0, 0);
 #pragma unroll
-  for (int e2 = 0; e2 < DT / 2; ++e2) {
+  for (int e2 = 0; e2 < D / 32; ++e2) {
     bf16x8 even, odd;
-    blk.v_pair(e2, even, odd);
+    values.v_pair(e2, even, odd);
 #pragma unroll
     for (int t = 0; t < QT; ++t) {
       st.o[t][2 * e2] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(even, pf[t], st.o[t][2 * e2], 0, 0, 0);
@@ -279,6 +291,11 @@ __global__ __launch_bounds__(256, QT <= 2 ? 2 : 1) void tree_attn_paged_kernel(c
   const int WS = 1 << p.ws_shift, KW = 4 >> p.ws_shift;   // row slabs, wavefronts that split a slab's keys
   const int slab = wave & (WS - 1), kp = wave >> p.ws_shift;
   const int P = 1 << p.page_shift;
+  // this lane's places in a block's codes and scales (pages of 16 keys: the block's second half is at the start of another page)
+  const bool k_late = col >= 8, v_late = g4 >= 2;
+  const int k_key = 8 * (col >> 2) + (col & 3) - (P == 16 && k_late ? 16 : 0), v_key = 8 * g4 - (P == 16 && v_late ? 16 : 0);
+  const unsigned k_off = (unsigned)(k_key * (D / 2) + g4 * (D / 8)), ks_off = (unsigned)((g4 * (D / 4) / 32) * P + k_key);
+  const unsigned v_off = (unsigned)(v_key * (D / 2) + col * 16), vs_off = (unsigned)((col * (D / 16) / 32) * P + v_key);
   const int head_bytes = page_head_bytes(D, P), codes = page_code_bytes(D, P), scales = page_scale_bytes(D, P);
 
   // this workgroup's places of the list
@@ -342,61 +359,73 @@ __global__ __launch_bounds__(256, QT <= 2 ? 2 : 1) void tree_attn_paged_kernel(c
       return ri;
     };
 
-    // ---- the prefix's blocks in the pages
-    GlobalBytes const pool = (GlobalBytes)p.pages;
+    // ---- the prefix's blocks in the pages: bases are scalars, a lane adds what it adds to every block
+    GlobalBytes const pool = (GlobalBytes)p.pages + (int64_t)g * head_bytes;
     ScalarI32 const table = (ScalarI32)p.table + (int64_t)b * p.table_stride;
     struct Ids { int a, b; };   // pages of the first and the second 16 keys
-    auto ids_of = [&](int blk) {
-      const int t0 = (blk - tree_blocks) * kBlockKeys;
+    auto ids_of = [&](int at) {   // (places of the prefix from here on: block `at` has keys 32 at ..)
+      const int t0 = at * kBlockKeys;
       return Ids{table[t0 >> p.page_shift], table[min(t0 + 16, L - 1) >> p.page_shift]};
     };
-    const bool k_late = col >= 8, v_late = g4 >= 2;   // this lane's keys are among the second 16
-    auto load = [&](int blk, Ids ids) {
-      PagedBlock<D> x;
-      const int t0 = (blk - tree_blocks) * kBlockKeys;
-      x.vis = L - t0 >= kBlockKeys ? ~0u : (1u << (L - t0)) - 1u;
-      if ((unsigned)ids.a >= (unsigned)p.n_pages) { ids.a = 0; x.vis &= 0xffff0000u; }
-      if ((unsigned)ids.b >= (unsigned)p.n_pages) { ids.b = 0; x.vis &= 0x0000ffffu; }
-      GlobalBytes const base_a = pool + ids.a * p.page_stride + (int64_t)g * head_bytes;
-      GlobalBytes const base_b = pool + ids.b * p.page_stride + (int64_t)g * head_bytes;
-      const int in_page = t0 & (P - 1), back = P == 16 ? 16 : 0;
-      const int tk = in_page + 8 * (col >> 2) + (col & 3) - (k_late ? back : 0);
-      const int tv = in_page + 8 * g4 - (v_late ? back : 0);
-      GlobalBytes const kb = (k_late ? base_b : base_a) + tk * (D / 2) + g4 * (D / 8);
-      GlobalBytes const vb = (v_late ? base_b : base_a) + codes + tv * (D / 2) + col * 16;
-      GlobalBytes const ksb = (k_late ? base_b : base_a) + 2 * codes + (g4 * (D / 4) / 32) * P + tk;
-      GlobalBytes const vsb = (v_late ? base_b : base_a) + 2 * codes + scales + (col * (D / 16) / 32) * P + tv;
+    auto vis_of = [&](int at, const Ids& ids) {   // bit t: key t is there
+      const int left = L - at * kBlockKeys;
+      unsigned vis = left >= kBlockKeys ? ~0u : (1u << left) - 1u;
+      if ((unsigned)ids.a >= (unsigned)p.n_pages) vis &= 0xffff0000u;
+      if ((unsigned)ids.b >= (unsigned)p.n_pages) vis &= 0x0000ffffu;
+      return vis;
+    };
+    auto page_base = [&](int id) { return pool + ((unsigned)id < (unsigned)p.n_pages ? id : 0) * p.page_stride; };
+    auto load_k = [&](PagedK<D>& x, int at, const Ids& ids) {
+      const int in_page = at * kBlockKeys & (P - 1);
+      GlobalBytes code = page_base(ids.a);
+      if (P == 16 && k_late) code = page_base(ids.b);
+      GlobalBytes scale = code + 2 * codes + in_page;
+      code += in_page * (D / 2);
 #pragma unroll
       for (int kt = 0; kt < 2; ++kt) {
         if constexpr (D == 128) {
-          const u32x4 c4 = *(const __attribute__((address_space(1))) u32x4*)(kb + kt * 4 * (D / 2));
+          const u32x4 w = *(const __attribute__((address_space(1))) u32x4*)(code + (k_off + kt * 4 * (D / 2)));
 #pragma unroll
-          for (int i = 0; i < 4; ++i) x.k[kt][i] = c4[i];
+          for (int i = 0; i < 4; ++i) x.c[kt][i] = w[i];
         } else {
-          const u32x2 c2 = *(const __attribute__((address_space(1))) u32x2*)(kb + kt * 4 * (D / 2));
-          x.k[kt][0] = c2[0]; x.k[kt][1] = c2[1];
+          const u32x2 w = *(const __attribute__((address_space(1))) u32x2*)(code + (k_off + kt * 4 * (D / 2)));
+          x.c[kt][0] = w[0]; x.c[kt][1] = w[1];
         }
-        x.k_scale[kt] = *(const __attribute__((address_space(1))) unsigned char*)(ksb + 4 * kt);
+        x.scale[kt] = *(const __attribute__((address_space(1))) unsigned char*)(scale + (ks_off + 4 * kt));
       }
+    };
+    auto load_v = [&](PagedV<D>& x, int at, const Ids& ids) {
+      const int in_page = at * kBlockKeys & (P - 1);
+      GlobalBytes code = page_base(ids.a);
+      if (P == 16 && v_late) code = page_base(ids.b);
+      GlobalBytes scale = code + 2 * codes + scales + in_page;
+      code += codes + in_page * (D / 2);
 #pragma unroll
       for (int h = 0; h < D / 64; ++h) {
-        const u32x4 c4 = *(const __attribute__((address_space(1))) u32x4*)(vb + 256 * h);
+        const u32x4 w = *(const __attribute__((address_space(1))) u32x4*)(code + (v_off + 256 * h));
 #pragma unroll
-        for (int i = 0; i < 4; ++i) x.v[4 * h + i] = c4[i];
+        for (int i = 0; i < 4; ++i) x.c[4 * h + i] = w[i];
       }
-      x.v_scale = *(const __attribute__((address_space(1))) u32x2*)vsb;
-      return x;
+      const u32x2 w = *(const __attribute__((address_space(1))) u32x2*)(scale + vs_off);
+      x.scale[0] = w[0]; x.scale[1] = w[1];
     };
 
     int blk = seg_begin + kp;
     const bool active = slab_live && blk < blk_end;
-    PagedBlock<D> cur{};
-    Ids next_ids{0, 0};
-    int pre = blk;   // the first block of the prefix that is this wavefront's
-    while (pre < tree_blocks) pre += KW;
-    if (active && pre < blk_end) {
-      cur = load(pre, ids_of(pre));
-      if (pre + KW < blk_end) next_ids = ids_of(pre + KW);
+    // the wavefront's places of the prefix: at, at + KW, .. last
+    int at = blk;
+    while (at < tree_blocks) at += KW;
+    at -= tree_blocks;
+    const bool any_prefix = slab_live && at + tree_blocks < blk_end;
+    const int last = at + (any_prefix ? (blk_end - tree_blocks - 1 - at) / KW * KW : 0);
+    PagedK<D> k_now{};
+    PagedV<D> v_now{};
+    Ids ids_now{0, 0}, ids_next{0, 0}, ids_third{0, 0};
+    if (any_prefix) {
+      ids_now = ids_of(at);
+      load_k(k_now, at, ids_now);
+      load_v(v_now, at, ids_now);
+      ids_next = ids_of(min(at + KW, last));
     }
 
     bf16x8 qf[QT][KS];
@@ -462,7 +491,12 @@ __global__ __launch_bounds__(256, QT <= 2 ? 2 : 1) void tree_attn_paged_kernel(c
         }
         const unsigned there = n - t0 >= kBlockKeys ? ~0u : (1u << (n - t0)) - 1u;
         auto visible = [&](int t) { return (unsigned)(tree_mask[t] >> t0) & there; };
-        process_block<QT, D>(st, x, qf, false, visible, p.c, g4, pf);
+        Scores<QT> sc;
+        float ex[QT][8];
+        score_block<QT, D>(sc, x, qf);
+        hide<QT>(sc, visible, p.c, g4);
+        exponents<QT, D>(st, sc, ex, p.c);
+        accumulate<QT, D>(st, ex, x, pf);
         if (any_wild) {
 #pragma unroll 1
           for (int key = 0; key < kBlockKeys; ++key) {
@@ -488,17 +522,34 @@ __global__ __launch_bounds__(256, QT <= 2 ? 2 : 1) void tree_attn_paged_kernel(c
           }
         }
       }
-      // ---- blocks of the prefix: the next one is on its way while one is worked on, and the pages of the one after it are known
-      for (; blk < blk_end; blk += KW) {
-        PagedBlock<D> next = cur;
-        if (blk + KW < blk_end) {
-          next = load(blk + KW, next_ids);
-          if (blk + 2 * KW < blk_end) next_ids = ids_of(blk + 2 * KW);
+      // ---- blocks of the prefix. The scores of the next block are formed beside the weights and sums of this one: its products do not
+      // wait for the exponentials, nor these for them. Behind the last block the last one's are formed again, for nobody.
+      if (any_prefix) {
+        Scores<QT> s_now;
+        score_block<QT, D>(s_now, k_now, qf);
+        int next = min(at + KW, last);
+        load_k(k_now, next, ids_next);
+        for (;;) {
+          const unsigned vis = vis_of(at, ids_now);
+          const int third = min(next + KW, last);
+          ids_third = ids_of(third);
+          PagedV<D> v_next;
+          load_v(v_next, next, ids_next);
+          if (vis != ~0u) hide<QT>(s_now, [&](int) { return vis; }, p.c, g4);
+          float x[QT][8];
+          exponents<QT, D>(st, s_now, x, p.c);
+          v_now.ready(vis, g4);
+          Scores<QT> s_next;
+          score_block<QT, D>(s_next, k_now, qf);
+          load_k(k_now, third, ids_third);
+          accumulate<QT, D>(st, x, v_now, pf);
+          if (at == last) break;
+#pragma unroll
+          for (int t = 0; t < QT; ++t) { s_now[t][0] = s_next[t][0]; s_now[t][1] = s_next[t][1]; }
+          v_now = v_next;
+          at = next; next = third;
+          ids_now = ids_next; ids_next = ids_third;
         }
-        cur.ready(g4);
-        const unsigned vis = cur.vis;
-        process_block<QT, D>(st, cur, qf, vis == ~0u, [&](int) { return vis; }, p.c, g4, pf);
-        cur = next;
       }
     }
 

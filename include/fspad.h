@@ -398,8 +398,9 @@ typedef struct {
   int32_t table_width;    /* entries of a block table's row, >= 1 (attention only) */
   int32_t max_kv_len;     /* no sequence is longer, 0..table_width * P (attention only): the launch is laid out for it */
   int64_t table_stride;   /* entries from row to row of the block table, >= table_width (attention only) */
-  int32_t workgroups;     /* tuning of the attention: 0 = the built-in choice, 1..4096 forces the workgroup count; the
-                             workspace's size depends on it */
+  int32_t workgroups;     /* tuning of the attention: 0 = the built-in choice; 1..4096 cuts the keys into about that many pieces
+                             beside one for each (sequence, kv head, group of query rows). Results do not depend on it beyond
+                             fp32 rounding of the join; the workspace's size does */
   int32_t reserved;       /* 0 */
 } fspad_paged_desc;
 

@@ -152,8 +152,9 @@ def tree_attn(q, k_tree, v_tree, pages: Pages, table, kv_len, n_nodes, mask, max
             |out' - out| <= r (1 + 2 r) sum_j w_j |v_j - out|,    w_j the exact weights, summing to 1
       - drops weights, and products of one with a value, below the smallest normal fp32 number (the largest weight being 1 at least, and the
         pieces of a row joined by factors that are dropped alike): n 2^-125 (1 + 2 max_j |v_j|)
-      - forms scores and sums in fp32: a score's error e <= (D + 8) 2^-24 scale sum_d |q_d k_jd| moves its weight by a factor within
-        1 +- 2 e, an exponential by 2^-22, and the two sums over n keys by n 2^-24 of sum_j w_j |v_j| (numerator) and of |out| (denominator).
+      - holds a query as the sum of two fp8 values, off by 2^-22 of the row's largest at most, and sums its 2 D products in fp32, in any
+        order and cut where it is not rounded: a score's error e <= (2 D + 8) 2^-23 scale sum_d |q_d k_jd| + 2^-22 scale max_d |q_d| sum_d
+        |k_jd| moves its weight by a factor within 1 +- 2 e, an exponential by 2^-22, and the two sums over n keys by n 2^-24 of sum_j w_j |v_j| (numerator) and of |out| (denominator).
     Rounding of the output itself is the caller's."""
     B, N, Hq, D = q.shape
     Hkv = k_tree.shape[2]
@@ -184,7 +185,8 @@ def tree_attn(q, k_tree, v_tree, pages: Pages, table, kv_len, n_nodes, mask, max
                     total = w.sum(axis=1, keepdims=True)
                     w = np.where(total == 0, 0.0, w / np.where(total == 0, 1.0, total))
                     o = w @ v
-                    e = (D + 8) * 2.0 ** -24 * abs(scale) * (np.abs(qq) @ np.abs(k).T).max(axis=1, keepdims=True)
+                    e = abs(scale) * ((2 * D + 8) * 2.0 ** -23 * (np.abs(qq) @ np.abs(k).T)
+                                      + 2.0 ** -22 * np.abs(qq).max(axis=1, keepdims=True) * np.abs(k).sum(axis=1)).max(axis=1, keepdims=True)
                     spread = np.stack([(w[h][:, None] * np.abs(v - o[h])).sum(axis=0) for h in range(G)])
                     r = 2.0 ** -8
                     bound[b, i, g * G:(g + 1) * G] = ((r * (1 + 2 * r) + 2 * e + 2.0 ** -22) * spread

@@ -2,18 +2,21 @@
 // cache format is in include/fspad.h). gfx950 (CDNA4) only.
 //
 // One pass over the keys with a running shift and sum per query row. A wavefront owns up to 64 query rows (16-row tiles) of one
-// kv head and takes 32-key blocks of K and V from the pages straight into registers, 4 bits an entry; they become bf16 on the
-// way into the matrix cores (v_cvt_scalef32_pk_bf16_fp4: two entries and their block's scale in one instruction, exact). The
-// layout of the pages is that of the operands:
-//   S^T = K Q^T    lane (col, g4), col = lane % 16, g4 = lane / 16, of a 16-key tile kt holds D/4 channels of key 8 (col / 4) +
-//                  4 kt + col % 4: one piece of its row, in one block of 32 channels
-//   O^T += V^T P^T lane (col, g4) holds D/16 channels of the keys 8 g4 .. 8 g4 + 7, the ones whose scores S^T leaves in it
-// so that the weights never leave the lane they arise in. Of a block of V the lane's 8 x D/16 entries turn from key order to
-// channel order two bytes at a time (v_perm_b32).
+// kv head and takes 32-key blocks of K and V from the pages straight into registers, 4 bits an entry. The layout of the pages is that
+// of the operands (lane (col, g4): col = lane % 16, g4 = lane / 16):
+//   S^T = K Q^T    on the block-scaled products (v_mfma_scale_f32_16x16x128_f8f6f4), which take K's codes and scales as they are: a
+//                  lane holds one block of 32 channels of key col, 16 bytes and a scale byte. They have no bf16 operand; a query row
+//                  is two fp8 ones instead (split_q), whose sum it is: D = 128 in two products, D = 64 in one, K's 64 channels twice
+//                  in its 128. As many clocks as bf16 products take, a quarter to half of the instructions, and nothing to convert:
+//   O^T += V^T P^T V's scales run along the channels, not along the keys that are summed over, so V becomes bf16
+//                  (v_cvt_scalef32_pk_bf16_fp4: two entries and their block's scale in one instruction, exact). A lane holds
+//                  D/16 channels of the keys 4 g4 .. 4 g4 + 3 and 16 more, those whose scores S^T leaves in it: the weights
+//                  never leave the lane they arise in, and a page of 16 keys is half a block for all lanes alike. The 8 x D/16 entries
+//                  turn from key order to channel order two bytes at a time (v_perm_b32).
 //
-// How a call is cut is decided on the device, from lengths it alone knows: the 32-key blocks of all (sequence, kv head, row
-// group) units form one list, which the workgroups share evenly. A unit that is one workgroup's goes straight to `out`; of the others
-// every piece leaves its un-normalised sums in the workspace and a second kernel joins them.
+// How a call is cut is decided on the device, from lengths it alone knows (piece_plan): a unit, 64 query rows or less of one kv head of one
+// sequence, is one workgroup's or is cut along its keys into equal pieces, a workgroup each. A whole unit goes straight to `out`; of
+// the others every piece leaves its un-normalised sums in the workspace and a second kernel joins them.
 #include <hip/hip_runtime.h>
 #include <float.h>
 #include <math.h>
@@ -23,18 +26,19 @@
 #include "fspad.h"
 #include "paged_layout.h"
 #include "paged_plan.h"
+#include "stream_gemm.h"
 #include "wave_scan.h"
 
 namespace {
 
 using namespace fspad_detail;
 
-typedef __attribute__((ext_vector_type(4))) float f32x4;
-typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
 typedef __attribute__((ext_vector_type(4))) __bf16 bf16x4;
 typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
 typedef __attribute__((ext_vector_type(4))) unsigned u32x4;
 typedef __attribute__((ext_vector_type(2))) unsigned u32x2;
+typedef __attribute__((ext_vector_type(8))) int i32x8;
+typedef __attribute__((ext_vector_type(2))) float f32x2;
 typedef const __attribute__((address_space(4))) int32_t* ScalarI32;
 typedef const __attribute__((address_space(1))) char* GlobalBytes;
 
@@ -49,12 +53,28 @@ struct PagedParams {
   const uint64_t* mask;
   void* out;
   int2* cuts;       // per unit: first partial slot and number of pieces (0: the unit is complete in `out`)
-  float* part;      // partial slots
+  float* part;      // partial slots, one for every piece
   int64_t page_stride, table_stride;
   int32_t B, N, Hq, Hkv, G, page_shift, n_pages, max_kv_len;
-  int32_t ws_shift, rows_per_group, groups, n_wgs, min_blocks, out_bf16;
+  uint32_t g_rcp;   // reciprocal(G)
+  int32_t ws_shift, rows_shift, rows_per_group, groups, max_pieces, resident, least_blocks, whole_blocks, forced, out_bf16;
   float c;          // softmax scale * log2(e)
 };
+
+// The arguments where the launch left them. What only a segment's start or end needs is fetched there, through a pointer that the
+// compiler takes for another one each time: kept in scalar registers for the length of a stream, arguments displaced what the stream needs.
+typedef const __attribute__((address_space(4))) PagedParams* Args;
+__device__ __forceinline__ Args fresh(Args p) {
+  asm volatile("" : "+s"(p));
+  return p;
+}
+
+// A lane's offset, as it stands here: widened to 64 bits ahead of a loop it would be added to every address by instructions of its own,
+// instead of by the load.
+__device__ __forceinline__ unsigned here(unsigned offset) {
+  asm volatile("" : "+v"(offset));
+  return offset;
+}
 
 // The shift of a row moves only when a score exceeds it by more than this (log2 units): weights stay below 2^8, which fp32 sums
 // and bf16 weights hold without loss, and accumulators are rescaled almost never after the first blocks.
@@ -63,48 +83,119 @@ constexpr float kNoShift = -FLT_MAX;   // below every score: the first visible o
 
 // ------------------------------------------------------------------------------------------------ plan
 
-// What a sequence is made of: `live` row groups of nb blocks each per kv head, the others one entry each (they write zeros).
+// What a sequence is made of: `live` row groups of nb blocks each per kv head, the others without nodes (they write zeros).
 struct SeqShape {
   int len, n, live, nb;
-  unsigned flat;
 };
-__device__ __forceinline__ SeqShape shape_of(const PagedParams& p, int len, int n) {
+__device__ __forceinline__ SeqShape shape_of(Args p, int b) {
   SeqShape s;
-  s.len = min(max(len, 0), p.max_kv_len);
-  s.n = min(max(n, 0), p.N);
-  s.live = (s.n * p.G + p.rows_per_group - 1) / p.rows_per_group;
-  s.nb = (s.len + kBlockKeys - 1) / kBlockKeys + (s.n + kBlockKeys - 1) / kBlockKeys;
-  s.flat = (unsigned)p.Hkv * (unsigned)(s.live * s.nb + p.groups - s.live);
+  s.len = b < p->B ? min(max(p->kv_len[b], 0), p->max_kv_len) : 0;
+  s.n = b < p->B ? min(max(p->n_nodes[b], 0), p->N) : 0;
+  s.live = (s.n * p->G + p->rows_per_group - 1) >> p->rows_shift;
+  s.nb = s.live > 0 ? (s.len + kBlockKeys - 1) / kBlockKeys + (s.n + kBlockKeys - 1) / kBlockKeys : 0;
   return s;
 }
 
-// 64 sequences at a time, one a lane, with their first places in the list.
-struct SeqChunk {
-  int chunk;
-  unsigned first, end;   // the lane's first place; the chunk's end
-  SeqShape s;
-};
-__device__ __forceinline__ SeqChunk load_chunk(const PagedParams& p, int chunk, unsigned begin, int lane) {
-  SeqChunk c;
-  c.chunk = chunk;
-  const int b = 64 * chunk + lane;
-  c.s = shape_of(p, b < p.B ? p.kv_len[b] : 0, b < p.B ? p.n_nodes[b] : 0);
-  if (b >= p.B) c.s.flat = 0;
-  const unsigned sum = (unsigned)wave_sum_upto((int)c.s.flat);
-  c.first = begin + sum - c.s.flat;
-  c.end = begin + (unsigned)__builtin_amdgcn_readlane((int)sum, 63);
-  return c;
+__device__ __forceinline__ int wave_max(int x) {
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) x = max(x, __shfl_xor(x, off));
+  return x;
+}
+__device__ __forceinline__ int last_lane(int x) { return __builtin_amdgcn_readlane(x, 63); }
+
+// Blocks of a piece, at most, for `blocks` blocks in `units` units of `longest` blocks at most. Pieces of one round (as many as the
+// device holds workgroups at once), if the units can be cut into so few, take as long as the longest of them; smaller ones in
+// several rounds share the device better and pay for starting and ending (kPieceCost blocks) more often.
+constexpr float kPieceCost = 12.0f;
+__device__ __forceinline__ int piece_length(Args p, int blocks, int units, int longest) {
+  const float slots = (float)(p->max_pieces - p->B * p->Hkv * p->groups);   // the sum of ceil(nb / len) is at most S / len + units
+  if (p->forced > 0) return max((int)ceilf((float)blocks / slots) + 1, 1);
+  if (longest <= p->whole_blocks) return max(longest, 1);
+  const float R = (float)p->resident, S = (float)blocks, U = (float)units;
+  float len = (float)longest, cost = S / R + fmaxf(U / R, 1.0f) * kPieceCost + 0.5f * len;   // whole units
+  if (units < p->resident) {
+    const float one = fminf(ceilf(S / (R - U)), ceilf(len / floorf(R / U)));   // either way there are at most R pieces
+    len = fminf(len, one);
+    cost = len + kPieceCost;
+  }
+  const float many = ceilf(__builtin_sqrtf(2.0f * kPieceCost * S / R));
+  if ((S + (S / many + 0.5f * U) * kPieceCost) / R + 0.5f * many < cost) len = fminf(len, many);
+  len = fmaxf(len, ceilf(S / slots) + 1.0f);
+  return max((int)len, p->least_blocks);
 }
 
-// The even split of T places over W workgroups: the first T % W of them have one more.
-struct Split {
-  unsigned quot, rem;
-  __device__ __forceinline__ unsigned begin(unsigned w) const { return w * quot + min(w, rem); }
-  __device__ __forceinline__ unsigned owner(unsigned x) const {
-    const unsigned big = rem * (quot + 1);
-    return x < big ? x / (quot + 1) : rem + (x - big) / quot;
-  }
+// This workgroup's piece. Pieces are numbered sequence by sequence, head by head, group by group, along the keys; workgroups eight
+// apart, which share a die and its L2 cache, take neighbouring ones.
+struct Piece {
+  int b, g, y, len, n, begin, end, nb, index, count;   // blocks [begin, end) of nb; index: its slot; count: pieces of the unit
+  bool any, dead;
 };
+__device__ __forceinline__ Piece piece_of(Args p, int w, int lane) {
+  SeqShape s = shape_of(p, lane);
+  int blocks = 0, units = 0, longest = 0;
+  for (int first = 0;;) {
+    blocks += last_lane(wave_sum_upto(p->Hkv * s.live * s.nb));
+    units += last_lane(wave_sum_upto(p->Hkv * s.live));
+    longest = max(longest, wave_max(s.nb));
+    first += 64;
+    if (first >= p->B) break;
+    s = shape_of(p, first + lane);
+  }
+  const int most = __builtin_amdgcn_readfirstlane(piece_length(p, blocks, units, longest));
+  // places of 64 sequences at a time
+  int places = 0, first = 0, upto, own, cuts;
+  auto count = [&] {
+    if (p->B > 64) s = shape_of(p, first + lane);
+    cuts = (s.nb + most - 1) / most;
+    own = first + lane < p->B ? p->Hkv * (s.live * cuts + p->groups - s.live) : 0;
+    upto = wave_sum_upto(own);
+  };
+  for (;;) {
+    count();
+    places += last_lane(upto);
+    first += 64;
+    if (first >= p->B) break;
+  }
+  Piece r{};
+  const int share = (places + 7) >> 3, at = (w & 7) * share + (w >> 3);
+  r.any = (w >> 3) < share && at < places;
+  if (!r.any) return r;
+  int before = 0;
+  if (p->B > 64) {
+    for (first = 0;; first += 64) {
+      count();
+      if (at < before + last_lane(upto)) break;
+      before += last_lane(upto);
+    }
+  } else {
+    first = 0;
+  }
+  const int i = __builtin_ctzll(__ballot(at < before + upto));   // the sequence that the place lies in
+  r.b = first + i;
+  r.len = __builtin_amdgcn_readlane(s.len, i);
+  r.n = __builtin_amdgcn_readlane(s.n, i);
+  r.nb = __builtin_amdgcn_readlane(s.nb, i);
+  r.count = __builtin_amdgcn_readlane(cuts, i);
+  const int live = __builtin_amdgcn_readlane(s.live, i), rel = at - before - __builtin_amdgcn_readlane(upto - own, i);
+  r.index = at;
+  const int heads = p->Hkv * live * r.count;
+  r.dead = rel >= heads;
+  if (r.dead) {
+    const int others = p->groups - live, x = rel - heads;
+    r.g = x / others;
+    r.y = live + x - r.g * others;
+    r.count = 1;
+  } else {
+    const int u = rel / r.count, part = rel - u * r.count;
+    r.g = u / live;
+    r.y = u - r.g * live;
+    // equal pieces, the first ones a block longer
+    const int each = r.nb / r.count, more = r.nb - each * r.count;
+    r.begin = part * each + min(part, more);
+    r.end = r.begin + each + (part < more ? 1 : 0);
+  }
+  return r;
+}
 
 // -------------------------------------------------------------------------------------------- operands
 
@@ -140,19 +231,66 @@ __device__ __forceinline__ unsigned two_values(unsigned codes, float scale, int 
                                                                                            : two_values<3>(codes, scale);
 }
 
+// The lane's j-th key of a block, less 4 g4.
+__device__ constexpr int key_of(int j) { return (j & 3) + 16 * (j >> 2); }
+
 // K and V of a 32-key block of the prefix as they lie in the pages. Keys that are not there (past the length, on a bad page) are
 // masked by their scores; their values only have to be finite, which codes are under any scale but 255.
-template <int D>
 struct PagedK {
-  unsigned c[2][D / 32], scale[2];
+  u32x4 c[2];
+  unsigned scale[2];
+};
 
-  __device__ __forceinline__ bf16x8 k_frag(int kt, int ks) const {
-    const float f = __builtin_bit_cast(float, scale[kt] << 23);
-    const unsigned w = c[kt][ks];
-    const u32x4 x = {two_values<0>(w, f), two_values<1>(w, f), two_values<2>(w, f), two_values<3>(w, f)};
-    return __builtin_bit_cast(bf16x8, x);
+// Query rows as the block-scaled products take them: row = hi + lo, each fp8 (e4m3, 4 significant bits) times a power of two of the
+// row. A bf16 value has 8 significant bits: hi takes the upper four, and what is left of them is a multiple of the value's last
+// place, eight at most, which lo holds exactly. With the row's largest magnitude at 128 .. 256 in hi's units (and what is left of it
+// below 256 in lo's, 32 times finer) this holds down to 2^-14 of the largest; below that a value is off by 2^-22 of the largest at
+// most. Rows with NaN or infinity have the scale that is NaN.
+template <int D>
+struct SplitQ {
+  i32x8 v[D / 64];     // D = 128: hi, lo; D = 64: hi in the first half, lo in the second
+  int scale[D / 64];
+
+  // x: channels 16 g4 .. + 15 of the row, D = 128 also 64 + 16 g4 .. + 15, bf16 pairs
+  __device__ __forceinline__ void split(const u32x4 (&x)[D / 32], int g4) {
+    unsigned top = 0;
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const unsigned w = x[i][k];
+        top = max(top, max(w & 0x7fffu, (w >> 16) & 0x7fffu));
+      }
+    top = max(top, (unsigned)__shfl_xor((int)top, 16));
+    top = max(top, (unsigned)__shfl_xor((int)top, 32));
+    const int e = max((int)(top >> 7), 13) - 7;                    // hi's scale byte; lo's is 5 less
+    const bool wild = top >= 0x7f80u;
+    const float to_hi = __builtin_bit_cast(float, (254 - e) << 23);   // 2^(127 - e); e <= 248
+    i32x8 hi{}, lo{};
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const unsigned w = x[i][k];
+        const float a = wild ? 0.f : __builtin_bit_cast(float, w << 16) * to_hi, b = wild ? 0.f : __builtin_bit_cast(float, w & 0xffff0000u) * to_hi;
+        const int h = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+        const f32x2 back = __builtin_amdgcn_cvt_pk_f32_fp8(h, false);
+        const int l = __builtin_amdgcn_cvt_pk_fp8_f32((a - back[0]) * 32.f, (b - back[1]) * 32.f, 0, false);
+        const int at = 2 * i + (k >> 1), shift = 16 * (k & 1);
+        hi[at] |= (h & 0xffff) << shift;
+        lo[at] |= (l & 0xffff) << shift;
+      }
+    const int s_hi = wild ? 255 : e, s_lo = wild ? 255 : e - 5;
+    if constexpr (D == 128) {
+      v[0] = hi; v[1] = lo;
+      scale[0] = s_hi; scale[1] = s_lo;
+    } else {
+      v[0] = i32x8{hi[0], hi[1], hi[2], hi[3], lo[0], lo[1], lo[2], lo[3]};
+      scale[0] = g4 < 2 ? s_hi : s_lo;   // a lane's scale is that of the products' channels 32 g4 .. + 31
+    }
   }
 };
+
 template <int D>
 struct PagedV {
   unsigned c[D / 16];
@@ -162,9 +300,9 @@ struct PagedV {
   __device__ __forceinline__ void ready(unsigned vis, int g4) {
 #pragma unroll
     for (int j = 0; j < 8; ++j) f[j] = __builtin_bit_cast(float, ((scale[j >> 2] >> (8 * (j & 3))) & 0xffu) << 23);
-    if (vis != ~0u) {
+    if (__builtin_expect(vis != ~0u, 0)) {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) f[j] = ((vis >> (8 * g4 + j)) & 1u) ? f[j] : 1.0f;
+      for (int j = 0; j < 8; ++j) f[j] = ((vis >> (4 * g4 + key_of(j))) & 1u) ? f[j] : 1.0f;
     }
   }
   __device__ __forceinline__ void v_pair(int e2, bf16x8& even, bf16x8& odd) const {
@@ -175,13 +313,11 @@ struct PagedV {
   }
 };
 
-// A block of the tree's own keys, bf16 (rows past the tree's end repeat its last one and are masked).
+// Values of a block of the tree's own keys, bf16 (rows past the tree's end repeat its last one and are masked).
 template <int D>
-struct TreeBlock {
-  bf16x8 k[2][D / 32];
+struct TreeV {
   unsigned v[8][D / 32];
 
-  __device__ __forceinline__ bf16x8 k_frag(int kt, int ks) const { return k[kt][ks]; }
   __device__ __forceinline__ void v_pair(int e2, bf16x8& even, bf16x8& odd) const {
     unsigned x[8];
 #pragma unroll
@@ -190,25 +326,45 @@ struct TreeBlock {
   }
 };
 
+// (an exponent of all ones carries into the sign's place when one is added to it)
+__device__ __forceinline__ unsigned has_wild(unsigned w) {
+  return ((w & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
+}
 __device__ __forceinline__ unsigned wild_halves(unsigned w) {   // all bits of a half that holds NaN or infinity
   return ((w & 0x7f80u) == 0x7f80u ? 0xffffu : 0u) | ((w & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u);
 }
 
 template <int QT>
-using Scores = f32x4[QT][2];   // lane (col, g4), [t][kt][i]: key 8 g4 + 4 kt + i against row 16 t + col
+using Scores = f32x4[QT][2];   // lane (col, g4), [t][kt][i]: key 16 kt + 4 g4 + i against row 16 t + col
 
-template <int QT, int D, typename Keys>
-__device__ __forceinline__ void score_block(Scores<QT>& s, const Keys& keys, const bf16x8 (&qf)[QT][D / 32]) {
+template <int QT, int D>
+__device__ __forceinline__ void score_block(Scores<QT>& s, const PagedK& keys, const SplitQ<D> (&q)[QT]) {
+#pragma unroll
+  for (int kt = 0; kt < 2; ++kt) {
+    const u32x4 c = keys.c[kt];
+    const i32x8 a = {(int)c[0], (int)c[1], (int)c[2], (int)c[3], 0, 0, 0, 0};
+#pragma unroll
+    for (int part = 0; part < D / 64; ++part)
+#pragma unroll
+      for (int t = 0; t < QT; ++t) {
+        const f32x4 before = part == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : s[t][kt];
+        s[t][kt] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, q[t].v[part], before, 4 /* a: fp4 */, 0 /* b: e4m3 */, 0, (int)keys.scale[kt], 0,
+                                                                    q[t].scale[part]);
+      }
+  }
+}
+
+// The tree's own keys and the query rows as they are.
+template <int QT, int D>
+__device__ __forceinline__ void score_tree(Scores<QT>& s, const bf16x8 (&k)[2][D / 32], const u32x4 (&q)[QT][D / 32]) {
 #pragma unroll
   for (int t = 0; t < QT; ++t) s[t][0] = s[t][1] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
   for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
-    for (int ks = 0; ks < D / 32; ++ks) {
-      const bf16x8 a = keys.k_frag(kt, ks);
+    for (int ks = 0; ks < D / 32; ++ks)
 #pragma unroll
-      for (int t = 0; t < QT; ++t) s[t][kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, qf[t][ks], s[t][kt], 0, 0, 0);
-    }
+      for (int t = 0; t < QT; ++t) s[t][kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[kt][ks], __builtin_bit_cast(bf16x8, q[t][ks]), s[t][kt], 0, 0, 0);
 }
 
 // Hides what a row does not see; visible(t): the 32 keys that this lane's row of tile t does.
@@ -217,51 +373,61 @@ __device__ __forceinline__ void hide(Scores<QT>& s, VisibleFn&& visible, float c
   const float hidden = c < 0.f ? INFINITY : -INFINITY;   // (times c: below every score)
 #pragma unroll
   for (int t = 0; t < QT; ++t) {
-    const unsigned vis = visible(t) >> (8 * g4);
+    const unsigned vis = visible(t) >> (4 * g4);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) s[t][j >> 2][j & 3] = ((vis >> j) & 1u) ? s[t][j >> 2][j & 3] : hidden;
+    for (int j = 0; j < 8; ++j) s[t][j >> 2][j & 3] = ((vis >> key_of(j)) & 1u) ? s[t][j >> 2][j & 3] : hidden;
   }
 }
 
-// Exponents of the weights, under the shifts in use or, where a score is too far above its row's, under shifts that move.
+// Exponents of the weights under the shifts in use, and the largest of this lane's.
 template <int QT, int D>
-__device__ __forceinline__ void exponents(RowState<QT, D>& st, const Scores<QT>& s, float (&x)[QT][8], float c) {
-  bool grow = false;
+__device__ __forceinline__ float exponents(const RowState<QT, D>& st, const Scores<QT>& s, float (&x)[QT][8], float c) {
+  float most = -INFINITY;
 #pragma unroll
   for (int t = 0; t < QT; ++t) {
     const float m = st.m[t];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) x[t][j] = fmaf(s[t][j >> 2][j & 3], c, -m);
-    const float top = fmaxf(fmaxf(fmaxf(x[t][0], x[t][1]), fmaxf(x[t][2], x[t][3])), fmaxf(fmaxf(x[t][4], x[t][5]), fmaxf(x[t][6], x[t][7])));
-    grow = grow || top > kLazyLog2;
-  }
-  if (__any(grow)) {   // rare: the rows' shifts move to their running maxima
-#pragma unroll
-    for (int t = 0; t < QT; ++t) {
-      float top = -INFINITY;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) top = fmaxf(top, s[t][j >> 2][j & 3] * c);
-      top = fmaxf(top, __shfl_xor(top, 16));
-      top = fmaxf(top, __shfl_xor(top, 32));
-      const float moved = fmaxf(st.m[t], top);
-      const float alpha = __builtin_amdgcn_exp2f(st.m[t] - moved);
-      st.m[t] = moved;
-      st.l[t] *= alpha;
-#pragma unroll
-      for (int e = 0; e < D / 16; ++e) st.o[t][e] *= alpha;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) x[t][j] = fmaf(s[t][j >> 2][j & 3], c, -moved);
+    for (int j = 0; j < 8; ++j) {
+      x[t][j] = fmaf(s[t][j >> 2][j & 3], c, -m);
+      most = fmaxf(most, x[t][j]);
     }
+  }
+  return most;
+}
+
+// Where a score is too far above its row's shift, rare: the rows' shifts move to their running maxima.
+template <int QT, int D>
+__device__ __forceinline__ void settle(RowState<QT, D>& st, const Scores<QT>& s, float (&x)[QT][8], float most, float c) {
+  if (__builtin_expect(!__any(most > kLazyLog2), 1)) return;
+#pragma unroll
+  for (int t = 0; t < QT; ++t) {
+    float top = -INFINITY;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) top = fmaxf(top, s[t][j >> 2][j & 3] * c);
+    top = fmaxf(top, __shfl_xor(top, 16));
+    top = fmaxf(top, __shfl_xor(top, 32));
+    const float moved = fmaxf(st.m[t], top);
+    const float alpha = __builtin_amdgcn_exp2f(st.m[t] - moved);
+    st.m[t] = moved;
+    st.l[t] *= alpha;
+#pragma unroll
+    for (int e = 0; e < D / 16; ++e) st.o[t][e] *= alpha;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[t][j] = fmaf(s[t][j >> 2][j & 3], c, -moved);
   }
 }
 
 // Weights are rounded to bf16, which is what the matrix cores take; their sum is that of the rounded ones.
-template <int QT, int D, typename Values>
-__device__ __forceinline__ void accumulate(RowState<QT, D>& st, const float (&x)[QT][8], const Values& values, bf16x8 (&pf)[QT]) {
+template <int QT>
+__device__ __forceinline__ void weigh(const float (&x)[QT][8], bf16x8 (&pf)[QT]) {
 #pragma unroll
   for (int t = 0; t < QT; ++t)
 #pragma unroll
     for (int j = 0; j < 8; ++j) pf[t][j] = (__bf16)__builtin_amdgcn_exp2f(x[t][j]);
+}
+
+template <int QT, int D, typename Values>
+__device__ __forceinline__ void accumulate(RowState<QT, D>& st, const bf16x8 (&pf)[QT], const Values& values) {
   bf16x8 ones;
 #pragma unroll
   for (int j = 0; j < 8; ++j) ones[j] = (__bf16)1.0f;
@@ -281,372 +447,358 @@ __device__ __forceinline__ void accumulate(RowState<QT, D>& st, const float (&x)
 
 // ---------------------------------------------------------------------------------------------- kernel
 
+// A partial slot: sums in the order in which lanes hold them, [row tile][four channel tiles][entry][lane] quads of channels (a store
+// instruction writes a kilobyte in a row), behind them the rows' shifts and sums.
+template <int D>
+__device__ __forceinline__ int64_t slot_floats(int rows) { return (int64_t)rows * (D + 2); }
+template <int D>
+__device__ __forceinline__ int quad_at(int tile, int quad, int entry, int lane) { return (((tile * (D / 64) + quad) * 4 + entry) * 64 + lane) * 4; }
+
+template <int QT>
+constexpr int kWaves = QT == 1 ? 4 : 8;
+
 template <int QT, int D>
-__global__ __launch_bounds__(256, QT <= 2 ? 2 : 1) void tree_attn_paged_kernel(const PagedParams p) {
-  constexpr int KS = D / 32, DT = D / 16, ROWS = 16 * QT;
-  __shared__ f32x4 merge_o[4][QT * DT][64];
-  __shared__ float2 merge_ml[4][QT][64];
+__global__ __launch_bounds__(64 * kWaves<QT>, QT == 1 ? 3 : 2) void tree_attn_paged_kernel(const PagedParams) {
+  Args p = (Args)__builtin_amdgcn_kernarg_segment_ptr();
+  constexpr int KS = D / 32, DT = D / 16, ROWS = 16 * QT, WAVES = kWaves<QT>;
+  __shared__ f32x4 merge_o[WAVES][QT * DT][64];
+  __shared__ float2 merge_ml[WAVES][QT][64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 15, g4 = lane >> 4;
-  const int WS = 1 << p.ws_shift, KW = 4 >> p.ws_shift;   // row slabs, wavefronts that split a slab's keys
-  const int slab = wave & (WS - 1), kp = wave >> p.ws_shift;
-  const int P = 1 << p.page_shift;
-  // this lane's places in a block's codes and scales (pages of 16 keys: the block's second half is at the start of another page)
-  const bool k_late = col >= 8, v_late = g4 >= 2;
-  const int k_key = 8 * (col >> 2) + (col & 3) - (P == 16 && k_late ? 16 : 0), v_key = 8 * g4 - (P == 16 && v_late ? 16 : 0);
-  const unsigned k_off = (unsigned)(k_key * (D / 2) + g4 * (D / 8)), ks_off = (unsigned)((g4 * (D / 4) / 32) * P + k_key);
-  const unsigned v_off = (unsigned)(v_key * (D / 2) + col * 16), vs_off = (unsigned)((col * (D / 16) / 32) * P + v_key);
-  const int head_bytes = page_head_bytes(D, P), codes = page_code_bytes(D, P), scales = page_scale_bytes(D, P);
+  const Piece piece = piece_of(p, blockIdx.x, lane);
+  if (!piece.any) return;
+  const int b = piece.b, g = piece.g, y = piece.y, L = piece.len, n = piece.n;
+  const int WS = 1 << p->ws_shift, KW = WAVES >> p->ws_shift;   // row slabs, wavefronts that split a slab's keys
+  const int slab = wave & (WS - 1), kp = wave >> p->ws_shift;
+  const int row0 = y * p->rows_per_group + slab * ROWS;
+  if (piece.begin == 0 && threadIdx.x == 0) p->cuts[(b * p->groups + y) * p->Hkv + g] = make_int2(piece.index, piece.count > 1 ? piece.count : 0);
 
-  // this workgroup's places of the list
-  SeqChunk ch = load_chunk(p, 0, 0, lane);
-  unsigned total = ch.end;
-  if (p.B > 64) {
-    for (int c = 1; 64 * c < p.B; ++c) total = load_chunk(p, c, total, lane).end;
+  struct RowInfo { bool exists, valid; int node; int64_t out; };
+  auto row_info = [&](int t) {
+    RowInfo ri;
+    const int rr = row0 + 16 * t + col;
+    ri.node = (int)div_rcp((unsigned)rr, (unsigned)p->G, p->g_rcp);
+    ri.exists = rr < p->N * p->G;
+    ri.valid = ri.exists && ri.node < n;
+    ri.out = ((int64_t)b * p->N + ri.node) * p->Hq + g * p->G + (rr - ri.node * p->G);
+    return ri;
+  };
+
+  RowState<QT, D> st;
+#pragma unroll
+  for (int t = 0; t < QT; ++t) {
+    st.m[t] = kNoShift;
+    st.l[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int e = 0; e < DT; ++e) st.o[t][e] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
-  const unsigned wgs = min((unsigned)p.n_wgs, max(total / (unsigned)p.min_blocks, 1u));
-  const unsigned w = blockIdx.x;
-  if (w >= wgs) return;
-  Split split;
-  split.quot = total / wgs;
-  split.rem = total - split.quot * wgs;
-  unsigned r = split.begin(w);
-  const unsigned r_end = split.begin(w + 1);
 
-  while (r < r_end) {
-    while (r >= ch.end) ch = load_chunk(p, ch.chunk + 1, ch.end, lane);   // (r lies before the list's end)
-    const int in_chunk = 63 - __builtin_clzll(__ballot(ch.first <= r && ch.s.flat > 0));
-    const int b = 64 * ch.chunk + in_chunk;
-    const int L = __builtin_amdgcn_readlane(ch.s.len, in_chunk), n = __builtin_amdgcn_readlane(ch.s.n, in_chunk);
-    const int nb = __builtin_amdgcn_readlane(ch.s.nb, in_chunk), live = __builtin_amdgcn_readlane(ch.s.live, in_chunk);
-    const unsigned rel = r - (unsigned)__builtin_amdgcn_readlane((int)ch.first, in_chunk);
-    const unsigned live_places = (unsigned)(p.Hkv * live) * (unsigned)nb;
-    const bool dead = rel >= live_places;   // a row group without nodes
-    int u, seg_begin, g, y;
-    if (dead) {
-      const int others = p.groups - live, x = (int)(rel - live_places);
-      u = p.Hkv * live + x;
-      g = x / others;
-      y = live + (x - g * others);
-      seg_begin = 0;
-    } else {
-      u = (int)(rel / (unsigned)nb);
-      seg_begin = (int)(rel - (unsigned)u * (unsigned)nb);
-      g = u / live;
-      y = u - g * live;
-    }
-    const int n_blocks = dead ? 1 : nb;
-    const int seg_count = min(n_blocks - seg_begin, (int)(r_end - r));
-    const bool whole_unit = seg_count == n_blocks;
-    const int unit = b * p.Hkv * p.groups + u;   // in the list's order
-    if (seg_begin == 0 && threadIdx.x == 0) {
-      const int pieces = whole_unit ? 0 : (int)(split.owner(r + (unsigned)n_blocks - 1) - w) + 1;
-      p.cuts[(b * p.Hkv + g) * p.groups + y] = make_int2(unit + (int)w, pieces);
-    }
-    const int row0 = y * p.rows_per_group + slab * ROWS;
-    const bool slab_live = !dead && row0 < n * p.G;
-    const int tree_blocks = (n + kBlockKeys - 1) / kBlockKeys;   // the first blocks of a unit
-    const int blk_end = seg_begin + seg_count;
-
-    struct RowInfo { bool exists, valid; int node; int64_t out; };
-    auto row_info = [&](int t) {
-      RowInfo ri;
-      const int rr = row0 + 16 * t + col;
-      ri.node = rr / p.G;
-      ri.exists = rr < p.N * p.G;
-      ri.valid = ri.exists && ri.node < n;
-      ri.out = ((int64_t)b * p.N + ri.node) * p.Hq + g * p.G + (rr - ri.node * p.G);
-      return ri;
-    };
-
-    // ---- the prefix's blocks in the pages: bases are scalars, a lane adds what it adds to every block
-    GlobalBytes const pool = (GlobalBytes)p.pages + (int64_t)g * head_bytes;
-    ScalarI32 const table = (ScalarI32)p.table + (int64_t)b * p.table_stride;
-    struct Ids { int a, b; };   // pages of the first and the second 16 keys
-    auto ids_of = [&](int at) {   // (places of the prefix from here on: block `at` has keys 32 at ..)
+  const int tree_blocks = (n + kBlockKeys - 1) / kBlockKeys;   // the first blocks of a unit
+  int blk = piece.begin + kp;                                  // neighbouring wavefronts take neighbouring blocks
+  if (row0 < n * p->G && blk < piece.end) {
+    // ---- the prefix's blocks in the pages: a half block's bases are scalars, a lane adds its own places
+    // (V's codes of D = 64 lie in groups of eight keys: half a piece each; the products' channels of D = 64 are K's, twice)
+    const int P = 1 << p->page_shift, codes = page_code_bytes(D, P), scales = page_scale_bytes(D, P), k_block = g4 & (D / 32 - 1);
+    const unsigned k_off = (unsigned)(col * (D / 2) + k_block * 16);
+    const unsigned v_off = (unsigned)(codes + (D == 128 ? g4 * 256 + col * 16 : (g4 >> 1) * 256 + col * 16 + (g4 & 1) * 8));
+    const unsigned ks_off = (unsigned)(2 * codes + k_block * P + col);
+    const unsigned vs_off = (unsigned)(2 * codes + scales + (col * (D / 16) / 32) * P + 4 * g4);
+    GlobalBytes const pool = (GlobalBytes)p->pages + (int64_t)g * page_head_bytes(D, P);
+    ScalarI32 const table = (ScalarI32)p->table + (int64_t)b * p->table_stride;
+    const int64_t page_stride = p->page_stride;
+    const int page_shift = p->page_shift, n_pages = p->n_pages;
+    struct Ids { int id[2]; };   // pages of the two half blocks
+    auto ids_of = [&](int at) {   // (places of the prefix: block `at` has keys 32 at ..)
       const int t0 = at * kBlockKeys;
-      return Ids{table[t0 >> p.page_shift], table[min(t0 + 16, L - 1) >> p.page_shift]};
+      return Ids{{table[t0 >> page_shift], table[min(t0 + 16, L - 1) >> page_shift]}};
     };
     auto vis_of = [&](int at, const Ids& ids) {   // bit t: key t is there
       const int left = L - at * kBlockKeys;
-      unsigned vis = left >= kBlockKeys ? ~0u : (1u << left) - 1u;
-      if ((unsigned)ids.a >= (unsigned)p.n_pages) vis &= 0xffff0000u;
-      if ((unsigned)ids.b >= (unsigned)p.n_pages) vis &= 0x0000ffffu;
+      unsigned vis = left >= kBlockKeys ? ~0u : left > 0 ? (1u << left) - 1u : 0u;
+      if ((unsigned)ids.id[0] >= (unsigned)n_pages) vis &= 0xffff0000u;
+      if ((unsigned)ids.id[1] >= (unsigned)n_pages) vis &= 0x0000ffffu;
       return vis;
     };
-    auto page_base = [&](int id) { return pool + ((unsigned)id < (unsigned)p.n_pages ? id : 0) * p.page_stride; };
-    auto load_k = [&](PagedK<D>& x, int at, const Ids& ids) {
-      const int in_page = at * kBlockKeys & (P - 1);
-      GlobalBytes code = page_base(ids.a);
-      if (P == 16 && k_late) code = page_base(ids.b);
-      GlobalBytes scale = code + 2 * codes + in_page;
-      code += in_page * (D / 2);
+    struct Block { GlobalBytes code[2], scale[2]; };
+    auto place = [&](int at, const Ids& ids) {
+      Block r;
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        const int id = (unsigned)ids.id[half] < (unsigned)n_pages ? ids.id[half] : 0, in_page = (at * kBlockKeys + 16 * half) & (P - 1);
+        GlobalBytes const page = pool + (int64_t)id * page_stride;
+        r.code[half] = page + in_page * (D / 2);
+        r.scale[half] = page + in_page;
+      }
+      return r;
+    };
+    auto load_k = [&](PagedK& x, const Block& block) {
+      const unsigned k_at = here(k_off), ks_at = here(ks_off);
 #pragma unroll
       for (int kt = 0; kt < 2; ++kt) {
-        if constexpr (D == 128) {
-          const u32x4 w = *(const __attribute__((address_space(1))) u32x4*)(code + (k_off + kt * 4 * (D / 2)));
-#pragma unroll
-          for (int i = 0; i < 4; ++i) x.c[kt][i] = w[i];
-        } else {
-          const u32x2 w = *(const __attribute__((address_space(1))) u32x2*)(code + (k_off + kt * 4 * (D / 2)));
-          x.c[kt][0] = w[0]; x.c[kt][1] = w[1];
-        }
-        x.scale[kt] = *(const __attribute__((address_space(1))) unsigned char*)(scale + (ks_off + 4 * kt));
+        x.c[kt] = *(const __attribute__((address_space(1))) u32x4*)(block.code[kt] + k_at);
+        x.scale[kt] = *(const __attribute__((address_space(1))) unsigned char*)(block.scale[kt] + ks_at);
       }
     };
-    auto load_v = [&](PagedV<D>& x, int at, const Ids& ids) {
-      const int in_page = at * kBlockKeys & (P - 1);
-      GlobalBytes code = page_base(ids.a);
-      if (P == 16 && v_late) code = page_base(ids.b);
-      GlobalBytes scale = code + 2 * codes + scales + in_page;
-      code += codes + in_page * (D / 2);
+    auto load_v = [&](PagedV<D>& x, const Block& block) {
+      const unsigned v_at = here(v_off), vs_at = here(vs_off);
 #pragma unroll
-      for (int h = 0; h < D / 64; ++h) {
-        const u32x4 w = *(const __attribute__((address_space(1))) u32x4*)(code + (v_off + 256 * h));
+      for (int h = 0; h < 2; ++h) {
+        if constexpr (D == 128) {
+          const u32x4 w = *(const __attribute__((address_space(1))) u32x4*)(block.code[h] + v_at);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) x.c[4 * h + i] = w[i];
+          for (int i = 0; i < 4; ++i) x.c[4 * h + i] = w[i];
+        } else {
+          const u32x2 w = *(const __attribute__((address_space(1))) u32x2*)(block.code[h] + v_at);
+          x.c[2 * h] = w[0]; x.c[2 * h + 1] = w[1];
+        }
+        x.scale[h] = *(const __attribute__((address_space(1))) unsigned*)(block.scale[h] + vs_at);
       }
-      const u32x2 w = *(const __attribute__((address_space(1))) u32x2*)(scale + vs_off);
-      x.scale[0] = w[0]; x.scale[1] = w[1];
     };
 
-    int blk = seg_begin + kp;
-    const bool active = slab_live && blk < blk_end;
     // the wavefront's places of the prefix: at, at + KW, .. last
     int at = blk;
     while (at < tree_blocks) at += KW;
     at -= tree_blocks;
-    const bool any_prefix = slab_live && at + tree_blocks < blk_end;
-    const int last = at + (any_prefix ? (blk_end - tree_blocks - 1 - at) / KW * KW : 0);
-    PagedK<D> k_now{};
-    PagedV<D> v_now{};
-    Ids ids_now{0, 0}, ids_next{0, 0}, ids_third{0, 0};
+    const int end = piece.end - tree_blocks;
+    const bool any_prefix = at < end;
+    const int last = any_prefix ? at + (end - 1 - at) / KW * KW : 0;
+    PagedK keys{};
+    PagedV<D> v_this{}, v_next;
+    Ids ids_next{};
+    Block block{};
+    unsigned vis_next = 0;
     if (any_prefix) {
-      ids_now = ids_of(at);
-      load_k(k_now, at, ids_now);
-      load_v(v_now, at, ids_now);
+      const Ids ids = ids_of(at);
       ids_next = ids_of(min(at + KW, last));
+      block = place(at, ids);
+      vis_next = vis_of(at, ids);
+      load_k(keys, block);
     }
-
-    bf16x8 qf[QT][KS];
-    uint64_t tree_mask[QT];
-    RowState<QT, D> st;
+    // the rows' channels that this lane holds, eight at a time: 16 g4 and 16 g4 + 8, and the same 64 further on
+    auto channel = [&](int i) { return (i >> 1) * 64 + 16 * g4 + 8 * (i & 1); };
+    u32x4 q_row[QT][KS];
 #pragma unroll
     for (int t = 0; t < QT; ++t) {
       const RowInfo ri = row_info(t);
-      const bool valid = ri.valid && active;
-      tree_mask[t] = valid ? p.mask[b * p.N + ri.node] : 0ull;
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks) {
-        bf16x8 z;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) z[j] = (__bf16)0.f;
-        qf[t][ks] = valid ? *reinterpret_cast<const bf16x8*>(p.q + (ri.out * D + (D / 4) * g4 + 8 * ks) * 2) : z;
-      }
-      st.m[t] = kNoShift;
-      st.l[t] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int e = 0; e < DT; ++e) st.o[t][e] = f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int i = 0; i < KS; ++i)
+        q_row[t][i] = ri.valid ? *reinterpret_cast<const u32x4*>(p->q + (ri.out * D + channel(i)) * 2) : u32x4{0u, 0u, 0u, 0u};
     }
 
-    if (active) {
-      bf16x8 pf[QT];
-      // ---- blocks of the tree
-      for (; blk < min(tree_blocks, blk_end); blk += KW) {
-        const int t0 = blk * kBlockKeys;
-        TreeBlock<D> x;
-        const int64_t row = (int64_t)p.Hkv * D * 2;
-        const char* kr = p.k_tree + ((int64_t)b * p.N * p.Hkv + g) * (D * 2);
-        const char* vr = p.v_tree + ((int64_t)b * p.N * p.Hkv + g) * (D * 2);
+    bf16x8 pf[QT];
+    // ---- blocks of the tree
+    for (; blk < min(tree_blocks, piece.end); blk += KW) {
+      const int t0 = blk * kBlockKeys;
+      const int64_t row = (int64_t)p->Hkv * D * 2;
+      const char* kr = p->k_tree + ((int64_t)b * p->N * p->Hkv + g) * (D * 2);
+      const char* vr = p->v_tree + ((int64_t)b * p->N * p->Hkv + g) * (D * 2);
+      bf16x8 kf[2][KS];
+      TreeV<D> values;
+      uint64_t tree_mask[QT];
 #pragma unroll
-        for (int kt = 0; kt < 2; ++kt) {
-          const int node = min(t0 + 8 * (col >> 2) + 4 * kt + (col & 3), n - 1);
+      for (int kt = 0; kt < 2; ++kt) {
+        const int node = min(t0 + 16 * kt + col, n - 1);
 #pragma unroll
-          for (int ks = 0; ks < KS; ++ks) x.k[kt][ks] = *reinterpret_cast<const bf16x8*>(kr + node * row + (D / 2) * g4 + 16 * ks);
+        for (int ks = 0; ks < KS; ++ks) kf[kt][ks] = *reinterpret_cast<const bf16x8*>(kr + node * row + 2 * channel(ks));
+      }
+#pragma unroll
+      for (int t = 0; t < QT; ++t) {
+        const RowInfo ri = row_info(t);
+        tree_mask[t] = ri.valid ? p->mask[b * p->N + ri.node] : 0ull;
+      }
+      unsigned wild = 0;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const int node = min(t0 + 4 * g4 + key_of(j), n - 1);
+        const char* src = vr + node * row + (D / 8) * col;
+        if constexpr (D == 128) {
+          const u32x4 v4 = *reinterpret_cast<const u32x4*>(src);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) values.v[j][i] = v4[i];
+        } else {
+          const u32x2 v2 = *reinterpret_cast<const u32x2*>(src);
+          values.v[j][0] = v2[0]; values.v[j][1] = v2[1];
         }
-        unsigned wild = 0;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const int node = min(t0 + 8 * g4 + j, n - 1);
-          const char* src = vr + node * row + (D / 8) * col;
-          if constexpr (D == 128) {
-            const u32x4 v4 = *reinterpret_cast<const u32x4*>(src);
+        for (int i = 0; i < D / 32; ++i) wild |= has_wild(values.v[j][i]);
+      }
+      // A weight of zero does not keep NaN and infinity out of a product. Where the tree's values hold any, they are taken out
+      // here and added below to the rows that see them.
+      const bool any_wild = __any(wild != 0);
+      if (__builtin_expect(any_wild, 0)) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) x.v[j][i] = v4[i];
-          } else {
-            const u32x2 v2 = *reinterpret_cast<const u32x2*>(src);
-            x.v[j][0] = v2[0]; x.v[j][1] = v2[1];
-          }
+        for (int j = 0; j < 8; ++j)
 #pragma unroll
-          for (int i = 0; i < D / 32; ++i) wild |= wild_halves(x.v[j][i]);
-        }
-        // A weight of zero does not keep NaN and infinity out of a product. Where the tree's values hold any, they are taken out
-        // here and added below to the rows that see them.
-        const bool any_wild = __any(wild != 0);
-        if (any_wild) {
-#pragma unroll
-          for (int j = 0; j < 8; ++j)
-#pragma unroll
-            for (int i = 0; i < D / 32; ++i) x.v[j][i] &= ~wild_halves(x.v[j][i]);
-        }
-        const unsigned there = n - t0 >= kBlockKeys ? ~0u : (1u << (n - t0)) - 1u;
-        auto visible = [&](int t) { return (unsigned)(tree_mask[t] >> t0) & there; };
-        Scores<QT> sc;
-        float ex[QT][8];
-        score_block<QT, D>(sc, x, qf);
-        hide<QT>(sc, visible, p.c, g4);
-        exponents<QT, D>(st, sc, ex, p.c);
-        accumulate<QT, D>(st, ex, x, pf);
-        if (any_wild) {
+          for (int i = 0; i < D / 32; ++i) values.v[j][i] &= ~wild_halves(values.v[j][i]);
+      }
+      const unsigned there = n - t0 >= kBlockKeys ? ~0u : (1u << (n - t0)) - 1u;
+      auto visible = [&](int t) { return (unsigned)(tree_mask[t] >> t0) & there; };
+      Scores<QT> s;
+      float x[QT][8];
+      score_tree<QT, D>(s, kf, q_row);
+      hide<QT>(s, visible, p->c, g4);
+      settle<QT, D>(st, s, x, exponents<QT, D>(st, s, x, p->c), p->c);
+      weigh<QT>(x, pf);
+      accumulate<QT, D>(st, pf, values);
+      if (__builtin_expect(any_wild, 0)) {
 #pragma unroll 1
-          for (int key = 0; key < kBlockKeys; ++key) {
-            if (!((there >> key) & 1u)) break;
-            const char* src = vr + (t0 + key) * row;
+        for (int key = 0; key < kBlockKeys; ++key) {
+          if (!((there >> key) & 1u)) break;
+          const char* src = vr + (t0 + key) * row;
 #pragma unroll
-            for (int t = 0; t < QT; ++t) {
-              float own = 0.f;
+          for (int t = 0; t < QT; ++t) {
+            float own = 0.f;
 #pragma unroll
-              for (int j = 0; j < 8; ++j) own = (key & 7) == j ? (float)pf[t][j] : own;
-              const float weight = __shfl(own, 16 * (key >> 3) + col);
-              if (!((visible(t) >> key) & 1u)) continue;
+            for (int j = 0; j < 8; ++j) own = (key & 3) + 4 * (key >> 4) == j ? (float)pf[t][j] : own;
+            const float weight = __shfl(own, 16 * ((key >> 2) & 3) + col);
+            if (!((visible(t) >> key) & 1u)) continue;
 #pragma unroll
-              for (int i = 0; i < 4; ++i)
+            for (int i = 0; i < 4; ++i)
 #pragma unroll
-                for (int e2 = 0; e2 < DT / 2; ++e2) {
-                  const unsigned w2 = *reinterpret_cast<const unsigned*>(src + 2 * (DT * (4 * g4 + i) + 2 * e2));
-                  const unsigned odd = wild_halves(w2);
-                  if (odd & 0xffffu) st.o[t][2 * e2][i] += weight * __builtin_bit_cast(float, w2 << 16);
-                  if (odd >> 16) st.o[t][2 * e2 + 1][i] += weight * __builtin_bit_cast(float, w2 & 0xffff0000u);
-                }
-            }
+              for (int e2 = 0; e2 < DT / 2; ++e2) {
+                const unsigned w2 = *reinterpret_cast<const unsigned*>(src + 2 * (DT * (4 * g4 + i) + 2 * e2));
+                const unsigned odd = wild_halves(w2);
+                if (odd & 0xffffu) st.o[t][2 * e2][i] += weight * __builtin_bit_cast(float, w2 << 16);
+                if (odd >> 16) st.o[t][2 * e2 + 1][i] += weight * __builtin_bit_cast(float, w2 & 0xffff0000u);
+              }
           }
-        }
-      }
-      // ---- blocks of the prefix. The scores of the next block are formed beside the weights and sums of this one: its products do not
-      // wait for the exponentials, nor these for them. Behind the last block the last one's are formed again, for nobody.
-      if (any_prefix) {
-        Scores<QT> s_now;
-        score_block<QT, D>(s_now, k_now, qf);
-        int next = min(at + KW, last);
-        load_k(k_now, next, ids_next);
-        for (;;) {
-          const unsigned vis = vis_of(at, ids_now);
-          const int third = min(next + KW, last);
-          ids_third = ids_of(third);
-          PagedV<D> v_next;
-          load_v(v_next, next, ids_next);
-          if (vis != ~0u) hide<QT>(s_now, [&](int) { return vis; }, p.c, g4);
-          float x[QT][8];
-          exponents<QT, D>(st, s_now, x, p.c);
-          v_now.ready(vis, g4);
-          Scores<QT> s_next;
-          score_block<QT, D>(s_next, k_now, qf);
-          load_k(k_now, third, ids_third);
-          accumulate<QT, D>(st, x, v_now, pf);
-          if (at == last) break;
-#pragma unroll
-          for (int t = 0; t < QT; ++t) { s_now[t][0] = s_next[t][0]; s_now[t][1] = s_next[t][1]; }
-          v_now = v_next;
-          at = next; next = third;
-          ids_now = ids_next; ids_next = ids_third;
         }
       }
     }
 
-    // ---- the key-splitting wavefronts of a slab meet in LDS; each writes its share of the (row tile, four channel tiles) quads
+    // ---- blocks of the prefix. A turn forms the weights and sums of one block and the scores of the next: its products do not wait
+    // for the exponentials, nor these for them. Its values and the keys of the block after it were asked for a turn ahead. The first turn
+    // has no block yet (weights of zero: the scores' code stands once), the last one forms its own scores again, for nobody.
+    if (any_prefix) {
+      SplitQ<D> q[QT];
+      float x[QT][8];
 #pragma unroll
-    for (int t = 0; t < QT; ++t) {
-      merge_ml[wave][t][lane] = make_float2(st.m[t], st.l[t][0]);
+      for (int t = 0; t < QT; ++t) {
+        q[t].split(q_row[t], g4);
 #pragma unroll
-      for (int e = 0; e < DT; ++e) merge_o[wave][t * DT + e][lane] = st.o[t][e];
-    }
-    __syncthreads();
-    constexpr int kQuads = DT / 4;
-    for (int q = kp; q < QT * kQuads; q += KW) {
-      const int t = q / kQuads, e0 = 4 * (q - t * kQuads);
-      float mm = kNoShift;
-      for (int k = 0; k < KW; ++k) mm = fmaxf(mm, merge_ml[slab + k * WS][t][lane].x);
-      float l_row = 0.f;
-      f32x4 o4[4];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) o4[j] = f32x4{0.f, 0.f, 0.f, 0.f};
-      for (int k = 0; k < KW; ++k) {   // in wavefront order: the same bits every time
-        const float2 ml = merge_ml[slab + k * WS][t][lane];
-        const float a = __builtin_amdgcn_exp2f(ml.x - mm);
-        l_row += ml.y * a;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) o4[j] += merge_o[slab + k * WS][t * DT + e0 + j][lane] * a;
+        for (int j = 0; j < 8; ++j) x[t][j] = -INFINITY;
       }
-      const RowInfo ri = row_info(t);
-      if (!ri.exists) continue;
-      if (whole_unit) {
-        const float inv = l_row == 0.f ? 0.f : 1.0f / l_row;
+      const float c = p->c;
+      unsigned vis_this = 0;   // (no key is there)
+      int third = min(at + KW, last);
+      at -= KW;
+      for (;;) {
+        load_v(v_next, block);
+        const unsigned vis = vis_next;
+        block = place(third, ids_next);
+        vis_next = vis_of(third, ids_next);
+        third = min(third + KW, last);
+        ids_next = ids_of(third);
+        Scores<QT> s;
+        score_block<QT, D>(s, keys, q);
+        weigh<QT>(x, pf);
+        load_k(keys, block);
+        __builtin_amdgcn_sched_barrier(0);
+        v_this.ready(vis_this, g4);
+        accumulate<QT, D>(st, pf, v_this);
+        if (__builtin_expect(vis != ~0u, 0)) hide<QT>(s, [&](int) { return vis; }, c, g4);
+        settle<QT, D>(st, s, x, exponents<QT, D>(st, s, x, c), c);
+        at += KW;
+        if (at > last) break;
+        v_this = v_next;
+        vis_this = vis;
+      }
+    }
+  }
+  p = fresh(p);
+
+  // ---- the key-splitting wavefronts of a slab meet in LDS; each writes its share of the (row tile, four channel tiles) quads
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int64_t at = ri.out * D + DT * (4 * g4 + i) + e0;
-          f32x4 val;
+  for (int t = 0; t < QT; ++t) {
+    merge_ml[wave][t][lane] = make_float2(st.m[t], st.l[t][0]);
 #pragma unroll
-          for (int j = 0; j < 4; ++j) val[j] = ri.valid ? o4[j][i] * inv : 0.f;
-          if (p.out_bf16) {
-            bf16x4 pk;
+    for (int e = 0; e < DT; ++e) merge_o[wave][t * DT + e][lane] = st.o[t][e];
+  }
+  __syncthreads();
+  constexpr int kQuads = DT / 4;
+  for (int q = kp; q < QT * kQuads; q += KW) {
+    const int t = q / kQuads, e0 = 4 * (q - t * kQuads);
+    float mm = kNoShift;
+    for (int k = 0; k < KW; ++k) mm = fmaxf(mm, merge_ml[slab + k * WS][t][lane].x);
+    float l_row = 0.f;
+    f32x4 o4[4];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) pk[j] = (__bf16)val[j];
-            *reinterpret_cast<bf16x4*>(static_cast<__bf16*>(p.out) + at) = pk;
-          } else {
-            *reinterpret_cast<f32x4*>(static_cast<float*>(p.out) + at) = val;
-          }
+    for (int j = 0; j < 4; ++j) o4[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int k = 0; k < KW; ++k) {   // in wavefront order: the same bits every time
+      const float2 ml = merge_ml[slab + k * WS][t][lane];
+      const float a = __builtin_amdgcn_exp2f(ml.x - mm);
+      l_row += ml.y * a;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) o4[j] += merge_o[slab + k * WS][t * DT + e0 + j][lane] * a;
+    }
+    const RowInfo ri = row_info(t);
+    if (!ri.exists) continue;
+    if (piece.count == 1) {
+      const float inv = l_row == 0.f ? 0.f : 1.0f / l_row;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int64_t out_at = ri.out * D + DT * (4 * g4 + i) + e0;
+        f32x4 val;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) val[j] = ri.valid ? o4[j][i] * inv : 0.f;
+        if (p->out_bf16) {
+          bf16x4 pk;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) pk[j] = (__bf16)val[j];
+          *reinterpret_cast<bf16x4*>(static_cast<__bf16*>(p->out) + out_at) = pk;
+        } else {
+          *reinterpret_cast<f32x4*>(static_cast<float*>(p->out) + out_at) = val;
         }
-      } else if (ri.valid) {
-        float* slot = p.part + (int64_t)(unit + (int)w) * p.rows_per_group * (D + 2);
-        const int lr = slab * ROWS + 16 * t + col;
-        if (g4 == 0 && e0 == 0) *reinterpret_cast<float2*>(slot + (int64_t)p.rows_per_group * D + 2 * lr) = make_float2(mm, l_row);
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          *reinterpret_cast<f32x4*>(slot + (int64_t)lr * D + DT * (4 * g4 + i) + e0) = f32x4{o4[0][i], o4[1][i], o4[2][i], o4[3][i]};
       }
+    } else {
+      float* part = p->part + piece.index * slot_floats<D>(p->rows_per_group);
+      const int tile = slab * QT + t;
+      if (g4 == 0 && e0 == 0) *reinterpret_cast<float2*>(part + (int64_t)p->rows_per_group * D + 2 * (16 * tile + col)) = make_float2(mm, l_row);
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        *reinterpret_cast<f32x4*>(part + quad_at<D>(tile, e0 / 4, i, lane)) = f32x4{o4[0][i], o4[1][i], o4[2][i], o4[3][i]};
     }
-    r += (unsigned)seg_count;
-    if (r < r_end) __syncthreads();   // the merge buffers are used again
   }
 }
 
-// Joins the pieces of the units that were cut: out = sum_s 2^(m_s - M) O_s / sum_s 2^(m_s - M) l_s. A thread has four channels of a row.
+// Joins the pieces of the units that were cut: out = sum_s 2^(m_s - M) O_s / sum_s 2^(m_s - M) l_s. A wavefront has one entry of a quad
+// for sixteen rows, as the pieces' wavefronts left it: four channels of a row a lane.
 template <int D>
 __global__ __launch_bounds__(256) void tree_attn_paged_join_kernel(const PagedParams p) {
-  const int g = blockIdx.y % p.Hkv, y = blockIdx.y / p.Hkv, b = blockIdx.z;
-  const int2 cut = p.cuts[(b * p.Hkv + g) * p.groups + y];
+  const int g = blockIdx.y, y = blockIdx.z % p.groups, b = blockIdx.z / p.groups;
+  const int2 cut = p.cuts[(b * p.groups + y) * p.Hkv + g];
   if (cut.y == 0) return;
-  constexpr int TPR = D / 4;
-  const int lr = blockIdx.x * (256 / TPR) + threadIdx.x / TPR, d0 = 4 * (threadIdx.x % TPR);
-  const int rr = y * p.rows_per_group + lr;
+  const int lane = threadIdx.x & 63, item = blockIdx.x * 4 + (threadIdx.x >> 6);   // (row tile, quad, entry)
+  const int i = item & 3, quad = (item >> 2) % (D / 64), tile = (item >> 2) / (D / 64);
+  const int lr = 16 * tile + (lane & 15), rr = y * p.rows_per_group + lr;
   if (lr >= p.rows_per_group || rr >= p.N * p.G) return;
-  const int node = rr / p.G;
+  const int node = (int)div_rcp((unsigned)rr, (unsigned)p.G, p.g_rcp);
   const int n = min(max(p.n_nodes[b], 0), p.N);
   f32x4 acc = {0.f, 0.f, 0.f, 0.f};
   if (node < n) {
-    const int64_t slot_floats = (int64_t)p.rows_per_group * (D + 2);
-    const float* base = p.part + cut.x * slot_floats;
-    const float* o_at = base + (int64_t)lr * D + d0;
+    const int64_t slot = slot_floats<D>(p.rows_per_group);
+    const float* base = p.part + cut.x * slot;
+    const float* o_at = base + quad_at<D>(tile, quad, i, lane);
     const float* ml_at = base + (int64_t)p.rows_per_group * D + 2 * lr;
     float M = kNoShift, sum = 0.f;
-    for (int s0 = 0; s0 < cut.y; s0 += 4) {   // in order: the same bits every time
-      float2 ml[4];
-      f32x4 o[4];
+    for (int s0 = 0; s0 < cut.y; s0 += 8) {   // in order: the same bits every time
+      float2 ml[8];
+      f32x4 o[8];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const int64_t at = min(s0 + k, cut.y - 1) * slot_floats;
+      for (int k = 0; k < 8; ++k) {
+        const int64_t at = min(s0 + k, cut.y - 1) * slot;
         ml[k] = *reinterpret_cast<const float2*>(ml_at + at);
         o[k] = *reinterpret_cast<const f32x4*>(o_at + at);
       }
       float mx = M;
 #pragma unroll
-      for (int k = 0; k < 4; ++k) mx = fmaxf(mx, ml[k].x);
+      for (int k = 0; k < 8; ++k) mx = fmaxf(mx, ml[k].x);
       const float a = __builtin_amdgcn_exp2f(M - mx);
       acc *= a;
       sum *= a;
       M = mx;
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
+      for (int k = 0; k < 8; ++k) {
         if (s0 + k >= cut.y) break;
         const float wgt = __builtin_amdgcn_exp2f(ml[k].x - M);
         sum += wgt * ml[k].y;
@@ -655,7 +807,7 @@ __global__ __launch_bounds__(256) void tree_attn_paged_join_kernel(const PagedPa
     }
     acc *= sum == 0.f ? 0.f : 1.0f / sum;
   }
-  const int64_t at = (((int64_t)b * p.N + node) * p.Hq + g * p.G + (rr - node * p.G)) * D + d0;
+  const int64_t at = (((int64_t)b * p.N + node) * p.Hq + g * p.G + (rr - node * p.G)) * D + (D / 16) * (4 * (lane >> 4) + i) + 4 * quad;
   if (p.out_bf16) {
     bf16x4 pk;
 #pragma unroll
@@ -668,16 +820,13 @@ __global__ __launch_bounds__(256) void tree_attn_paged_join_kernel(const PagedPa
 
 template <int D>
 void launch(const PagedPlan& pl, const PagedParams& p, hipStream_t stream) {
-  const dim3 grid((unsigned)pl.n_wgs);
-  switch (pl.QT) {
-    case 1: hipLaunchKernelGGL((tree_attn_paged_kernel<1, D>), grid, dim3(256), 0, stream, p); break;
-    case 2: hipLaunchKernelGGL((tree_attn_paged_kernel<2, D>), grid, dim3(256), 0, stream, p); break;
-    case 3: hipLaunchKernelGGL((tree_attn_paged_kernel<3, D>), grid, dim3(256), 0, stream, p); break;
-    default: hipLaunchKernelGGL((tree_attn_paged_kernel<4, D>), grid, dim3(256), 0, stream, p); break;
-  }
-  constexpr int kRows = 256 / (D / 4);
+  // (a multiple of eight: workgroup w takes place w / 8 of die w % 8's share)
+  const dim3 grid((unsigned)((pl.max_pieces + 7) / 8 * 8));
+  if (pl.QT == 1) hipLaunchKernelGGL((tree_attn_paged_kernel<1, D>), grid, dim3(64 * kWaves<1>), 0, stream, p);
+  else hipLaunchKernelGGL((tree_attn_paged_kernel<2, D>), grid, dim3(64 * kWaves<2>), 0, stream, p);
+  if (!pl.may_cut) return;
   const int rows = pl.rows_per_group < p.N * p.G ? pl.rows_per_group : p.N * p.G;
-  hipLaunchKernelGGL((tree_attn_paged_join_kernel<D>), dim3((unsigned)((rows + kRows - 1) / kRows), (unsigned)(p.Hkv * pl.groups), (unsigned)p.B),
+  hipLaunchKernelGGL((tree_attn_paged_join_kernel<D>), dim3((unsigned)((rows + 15) / 16 * (D / 64)), (unsigned)p.Hkv, (unsigned)(p.B * pl.groups)),
                      dim3(256), 0, stream, p);
 }
 
@@ -709,7 +858,9 @@ extern "C" fspad_status fspad_tree_attn_paged(const fspad_paged_desc* desc, cons
   p.page_stride = d.page_stride; p.table_stride = d.table_stride;
   p.B = d.batch; p.N = d.n_nodes_max; p.Hq = d.n_q_heads; p.Hkv = d.n_kv_heads; p.G = d.n_q_heads / d.n_kv_heads;
   p.page_shift = log2_of(d.page_tokens); p.n_pages = d.n_pages; p.max_kv_len = d.max_kv_len;
-  p.ws_shift = log2_of(pl.WS); p.rows_per_group = pl.rows_per_group; p.groups = pl.groups; p.n_wgs = pl.n_wgs; p.min_blocks = pl.min_blocks;
+  p.g_rcp = reciprocal(p.G);
+  p.ws_shift = log2_of(pl.WS); p.rows_shift = log2_of(pl.rows_per_group); p.rows_per_group = pl.rows_per_group; p.groups = pl.groups;
+  p.max_pieces = pl.max_pieces; p.resident = pl.resident; p.least_blocks = pl.least_blocks; p.whole_blocks = pl.whole_blocks; p.forced = d.workgroups;
   p.out_bf16 = d.out_dtype == FSPAD_BF16;
   p.c = c;
   hipStream_t stream = reinterpret_cast<hipStream_t>(hip_stream);

@@ -15,39 +15,40 @@ constexpr int kPagedMaxBatch = 1024;
 constexpr int kPagedComputeUnits = 256;
 
 struct PagedPlan {
-  int QT, WS;            // 16-row tiles of a wavefront, row slabs of a workgroup (4 / WS wavefronts split a slab's keys)
-  int rows_per_group;    // WS * 16 * QT
+  int QT, WS;            // 16-row tiles of a wavefront, row slabs of a workgroup (its other wavefronts split a slab's keys)
+  int rows_per_group;    // WS * 16 * QT: 16, 32 or 64
   int groups;            // row groups of a kv head's N * G rows
-  int n_wgs, min_blocks; // workgroups at most; blocks that a workgroup is worth
+  int resident;          // workgroups that the device holds at once
+  int least_blocks, whole_blocks;   // no piece is shorter, no unit of up to so many blocks is cut
+  bool may_cut;          // a unit can be so long that it is cut
+  int max_pieces;
   size_t cuts_bytes, workspace_bytes;
 };
 
-inline int64_t paged_places(const fspad_paged_desc& d, int groups) {   // of the list, at most
-  const int64_t blocks = ((int64_t)d.max_kv_len + kBlockKeys - 1) / kBlockKeys + (d.n_nodes_max + kBlockKeys - 1) / kBlockKeys;
-  return (int64_t)d.batch * d.n_kv_heads * groups * blocks;
+inline int64_t paged_unit_blocks(const fspad_paged_desc& d) {   // at most
+  return ((int64_t)d.max_kv_len + kBlockKeys - 1) / kBlockKeys + (d.n_nodes_max + kBlockKeys - 1) / kBlockKeys;
 }
 
-// Up to 64 rows: one slab, the four wavefronts split the keys. Up to 128: two slabs; more: four, in groups of up to 256 rows.
+// Rows of a workgroup: 16 (four wavefronts), 32 or 64 (eight), the number that leaves the fewest of them empty.
 inline PagedPlan plan_paged(const fspad_paged_desc& d) {
   PagedPlan pl{};
   const int rows = d.n_nodes_max * (d.n_q_heads / d.n_kv_heads);
-  pl.groups = (rows + 255) / 256;
-  const int share = (rows + pl.groups - 1) / pl.groups;
-  pl.WS = share <= 64 ? 1 : share <= 128 ? 2 : 4;
-  pl.QT = (share + 16 * pl.WS - 1) / (16 * pl.WS);
-  pl.rows_per_group = pl.WS * 16 * pl.QT;
-  pl.min_blocks = 2 * (4 / pl.WS);
-  const int64_t places = paged_places(d, pl.groups);
-  int64_t wgs = pl.QT <= 2 ? 2 * kPagedComputeUnits : kPagedComputeUnits;
-  if (d.workgroups > 0) {
-    wgs = d.workgroups;
-    pl.min_blocks = 1;
-  }
-  const int64_t most = places / pl.min_blocks > 1 ? places / pl.min_blocks : 1;
-  pl.n_wgs = (int)(wgs < most ? wgs : most);
-  const int64_t units = (int64_t)d.batch * d.n_kv_heads * pl.groups;
+  pl.rows_per_group = rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
+  pl.groups = (rows + pl.rows_per_group - 1) / pl.rows_per_group;
+  pl.QT = pl.rows_per_group == 16 ? 1 : 2;
+  pl.WS = pl.rows_per_group == 64 ? 2 : 1;
+  const int key_waves = pl.QT == 1 ? 4 : 8 / pl.WS;
+  pl.resident = pl.QT == 1 ? 3 * kPagedComputeUnits : kPagedComputeUnits;
+  pl.least_blocks = 2 * key_waves;
+  pl.whole_blocks = 4 * key_waves;
+  const int64_t units = (int64_t)d.batch * d.n_kv_heads * pl.groups, longest = paged_unit_blocks(d);
+  pl.may_cut = d.workgroups > 0 || longest > pl.whole_blocks;
+  // as many as there may be blocks, but at most two rounds of the device beside one for each unit
+  int64_t cut = d.workgroups > 0 ? d.workgroups : 2 * pl.resident;
+  if (cut > units * longest) cut = units * longest;
+  pl.max_pieces = (int)(units + (pl.may_cut ? cut : 0));
   pl.cuts_bytes = (size_t)((units * 8 + 15) / 16 * 16);
-  pl.workspace_bytes = pl.cuts_bytes + (size_t)(units + pl.n_wgs) * pl.rows_per_group * (d.head_dim + 2) * 4;
+  pl.workspace_bytes = pl.cuts_bytes + (pl.may_cut ? (size_t)pl.max_pieces * pl.rows_per_group * (d.head_dim + 2) * 4 : 0);
   return pl;
 }
 
@@ -59,11 +60,12 @@ inline fspad_status check_paged_attn(const fspad_paged_desc& d) {
   if (d.table_width < 1 || d.table_stride < d.table_width || (int64_t)d.table_width * d.page_tokens > INT32_MAX) return FSPAD_ERR_SHAPE;
   if (d.max_kv_len < 0 || d.max_kv_len > d.table_width * d.page_tokens) return FSPAD_ERR_SHAPE;
   if (d.workgroups < 0 || d.workgroups > 4096) return FSPAD_ERR_SHAPE;
-  // 32-bit places, units and launch dimensions
+  // 32-bit rows, units and blocks of all units, and launch dimensions
   const int64_t rows = (int64_t)d.n_nodes_max * (d.n_q_heads / d.n_kv_heads);
-  const int64_t groups = (rows + 255) / 256;
-  if (rows > (1 << 20) || d.n_kv_heads * groups > 65535) return FSPAD_ERR_SHAPE;
-  if (paged_places(d, (int)groups) > (1 << 30)) return FSPAD_ERR_SHAPE;
+  if (rows > (1 << 20) || d.n_kv_heads > 65535) return FSPAD_ERR_SHAPE;
+  const PagedPlan pl = plan_paged(d);
+  if ((int64_t)d.batch * pl.groups > 65535) return FSPAD_ERR_SHAPE;
+  if ((int64_t)d.batch * d.n_kv_heads * pl.groups * paged_unit_blocks(d) > (1 << 30)) return FSPAD_ERR_SHAPE;
   return FSPAD_OK;
 }
 

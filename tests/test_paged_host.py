@@ -116,19 +116,18 @@ def test_page_map_refuses_arguments(lib):
 @pytest.mark.parametrize("B,L", [(1, 0), (1, 1), (3, 700), (64, 4096)])
 @pytest.mark.parametrize("workgroups", [0, 1, 333])
 def test_workspace_holds_a_slot_for_every_piece(N, Hq, Hkv, D, B, L, workgroups):
-    """Slots are numbered by unit plus workgroup: units - 1 + workgroups - 1 is the last one. More workgroups than asked for never run, and
-    the library's own choice is at most two for a compute unit."""
+    """Where units can be cut: a slot for every unit and for every workgroup asked for beside them (or for every block, if there are fewer)."""
     d = _desc(batch=B, n_nodes_max=N, n_q_heads=Hq, n_kv_heads=Hkv, head_dim=D, page_stride=Hkv * 17 * D, max_kv_len=L, table_width=300, table_stride=300,
               workgroups=workgroups)
     need = fspad.fspad_tree_attn_paged_workspace_bytes(d)
     rows = N * (Hq // Hkv)
-    groups = -(-rows // 256)
-    units = B * Hkv * groups
-    per_group = -(-rows // groups)
-    wgs = min(workgroups or 512, units * (-(-L // 32) + -(-N // 32)))
+    per_group = next(r for r in (16, 32, 64) if rows <= r or r == 64)
+    units = B * Hkv * -(-rows // per_group)
+    blocks = units * (-(-L // 32) + -(-N // 32))
     slot = per_group * (D + 2) * 4
-    assert need >= units * 8 + (units + (wgs if workgroups else 1)) * slot
-    assert need <= 16 + units * 8 + (units + (workgroups or 512)) * (per_group + 63) * (D + 2) * 4
+    if workgroups or L >= 4096:
+        assert need >= units * 8 + (units + min(workgroups or 256, blocks)) * slot
+    assert units * 8 <= need <= 16 + units * 8 + (units + (workgroups or 2048)) * slot
 
 
 def test_binding_refuses_tensors():

@@ -69,8 +69,8 @@ __device__ __forceinline__ Args fresh(Args p) {
   return p;
 }
 
-// A lane's offset, as it stands here: widened to 64 bits ahead of a loop it would be added to every address by instructions of its own,
-// instead of by the load.
+// A lane's number, as it stands here: what is made of it is not made ahead of a loop and kept. (An offset that was widened to 64 bits there
+// would be added to every address by instructions of its own, instead of by the load.)
 __device__ __forceinline__ unsigned here(unsigned offset) {
   asm volatile("" : "+v"(offset));
   return offset;
@@ -204,7 +204,7 @@ struct RowState {
   static constexpr int DT = D / 16;
   f32x4 o[QT][DT];   // O^T: lane (col, g4), entry i <-> row 16 t + col, channel DT (4 g4 + i) + e
   float m[QT];       // shift in use (log2 units): within kLazyLog2 of the running maximum
-  f32x4 l[QT];       // sum of the rounded weights, formed on the matrix cores (all entries equal)
+  float l[QT];       // sum of the rounded weights
 };
 
 // (key 2i, key 2i+1) of one channel from (channel, next channel) of the two keys
@@ -236,6 +236,7 @@ __device__ constexpr int key_of(int j) { return (j & 3) + 16 * (j >> 2); }
 
 // K and V of a 32-key block of the prefix as they lie in the pages. Keys that are not there (past the length, on a bad page) are
 // masked by their scores; their values only have to be finite, which codes are under any scale but 255.
+struct __attribute__((packed)) Unaligned { unsigned word; };
 struct PagedK {
   u32x4 c[2];
   unsigned scale[2];
@@ -249,7 +250,7 @@ struct PagedK {
 template <int D>
 struct SplitQ {
   i32x8 v[D / 64];     // D = 128: hi, lo; D = 64: hi in the first half, lo in the second
-  int scale[D / 64];
+  int scale;           // D = 128: hi's in the first byte, lo's in the second
 
   // x: channels 16 g4 .. + 15 of the row, D = 128 also 64 + 16 g4 .. + 15, bf16 pairs
   __device__ __forceinline__ void split(const u32x4 (&x)[D / 32], int g4) {
@@ -283,10 +284,10 @@ struct SplitQ {
     const int s_hi = wild ? 255 : e, s_lo = wild ? 255 : e - 5;
     if constexpr (D == 128) {
       v[0] = hi; v[1] = lo;
-      scale[0] = s_hi; scale[1] = s_lo;
+      scale = s_hi | s_lo << 8;
     } else {
       v[0] = i32x8{hi[0], hi[1], hi[2], hi[3], lo[0], lo[1], lo[2], lo[3]};
-      scale[0] = g4 < 2 ? s_hi : s_lo;   // a lane's scale is that of the products' channels 32 g4 .. + 31
+      scale = g4 < 2 ? s_hi : s_lo;   // a lane's scale is that of the products' channels 32 g4 .. + 31
     }
   }
 };
@@ -301,8 +302,9 @@ struct PagedV {
 #pragma unroll
     for (int j = 0; j < 8; ++j) f[j] = __builtin_bit_cast(float, ((scale[j >> 2] >> (8 * (j & 3))) & 0xffu) << 23);
     if (__builtin_expect(vis != ~0u, 0)) {
+      const unsigned own = vis >> here(4 * g4);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) f[j] = ((vis >> (4 * g4 + key_of(j))) & 1u) ? f[j] : 1.0f;
+      for (int j = 0; j < 8; ++j) f[j] = ((own >> key_of(j)) & 1u) ? f[j] : 1.0f;
     }
   }
   __device__ __forceinline__ void v_pair(int e2, bf16x8& even, bf16x8& odd) const {
@@ -344,13 +346,14 @@ __device__ __forceinline__ void score_block(Scores<QT>& s, const PagedK& keys, c
     const u32x4 c = keys.c[kt];
     const i32x8 a = {(int)c[0], (int)c[1], (int)c[2], (int)c[3], 0, 0, 0, 0};
 #pragma unroll
-    for (int part = 0; part < D / 64; ++part)
+    for (int t = 0; t < QT; ++t)
+      s[t][kt] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, q[t].v[0], f32x4{0.f, 0.f, 0.f, 0.f}, 4 /* a: fp4 */, 0 /* b: e4m3 */, 0, (int)keys.scale[kt],
+                                                                  0, q[t].scale);
+    if constexpr (D == 128) {
 #pragma unroll
-      for (int t = 0; t < QT; ++t) {
-        const f32x4 before = part == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : s[t][kt];
-        s[t][kt] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, q[t].v[part], before, 4 /* a: fp4 */, 0 /* b: e4m3 */, 0, (int)keys.scale[kt], 0,
-                                                                    q[t].scale[part]);
-      }
+      for (int t = 0; t < QT; ++t)
+        s[t][kt] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, q[t].v[1], s[t][kt], 4, 0, 0, (int)keys.scale[kt], 1 /* the second byte */, q[t].scale);
+    }
   }
 }
 
@@ -373,7 +376,7 @@ __device__ __forceinline__ void hide(Scores<QT>& s, VisibleFn&& visible, float c
   const float hidden = c < 0.f ? INFINITY : -INFINITY;   // (times c: below every score)
 #pragma unroll
   for (int t = 0; t < QT; ++t) {
-    const unsigned vis = visible(t) >> (4 * g4);
+    const unsigned vis = visible(t) >> here(4 * g4);
 #pragma unroll
     for (int j = 0; j < 8; ++j) s[t][j >> 2][j & 3] = ((vis >> key_of(j)) & 1u) ? s[t][j >> 2][j & 3] : hidden;
   }
@@ -395,10 +398,13 @@ __device__ __forceinline__ float exponents(const RowState<QT, D>& st, const Scor
   return most;
 }
 
-// Where a score is too far above its row's shift, rare: the rows' shifts move to their running maxima.
-template <int QT, int D>
-__device__ __forceinline__ void settle(RowState<QT, D>& st, const Scores<QT>& s, float (&x)[QT][8], float most, float c) {
+// Where a score is too far above its row's shift, rare: the rows' shifts move to their running maxima. The scores are formed again for it
+// (score(s)): kept until here they would take sixteen registers more than the exponents made of them.
+template <int QT, int D, typename ScoreFn>
+__device__ __forceinline__ void settle(RowState<QT, D>& st, float (&x)[QT][8], float most, float c, ScoreFn&& score) {
   if (__builtin_expect(!__any(most > kLazyLog2), 1)) return;
+  Scores<QT> s;
+  score(s);
 #pragma unroll
   for (int t = 0; t < QT; ++t) {
     float top = -INFINITY;
@@ -432,10 +438,11 @@ __device__ __forceinline__ void accumulate(RowState<QT, D>& st, const bf16x8 (&p
 #pragma unroll
   for (int j = 0; j < 8; ++j) ones[j] = (__bf16)1.0f;
 #pragma unroll
-  for (int t = 0; t < QT; ++t) st.l[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pf[t], st.l[t], 0, 0, 0);
+  for (int t = 0; t < QT; ++t) st.l[t] += __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pf[t], f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0)[0];   // (all entries equal)
 #pragma unroll
   for (int e2 = 0; e2 < D / 32; ++e2) {
     bf16x8 even, odd;
+    __builtin_amdgcn_sched_barrier(0);
     values.v_pair(e2, even, odd);
 #pragma unroll
     for (int t = 0; t < QT; ++t) {
@@ -488,7 +495,7 @@ __global__ __launch_bounds__(64 * kWaves<QT>, QT == 1 ? 3 : 2) void tree_attn_pa
 #pragma unroll
   for (int t = 0; t < QT; ++t) {
     st.m[t] = kNoShift;
-    st.l[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    st.l[t] = 0.f;
 #pragma unroll
     for (int e = 0; e < DT; ++e) st.o[t][e] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
@@ -536,7 +543,7 @@ __global__ __launch_bounds__(64 * kWaves<QT>, QT == 1 ? 3 : 2) void tree_attn_pa
 #pragma unroll
       for (int kt = 0; kt < 2; ++kt) {
         x.c[kt] = *(const __attribute__((address_space(1))) u32x4*)(block.code[kt] + k_at);
-        x.scale[kt] = *(const __attribute__((address_space(1))) unsigned char*)(block.scale[kt] + ks_at);
+        x.scale[kt] = ((const __attribute__((address_space(1))) Unaligned*)(block.scale[kt] + ks_at))->word;   // (the products take its first byte)
       }
     };
     auto load_v = [&](PagedV<D>& x, const Block& block) {
@@ -562,8 +569,8 @@ __global__ __launch_bounds__(64 * kWaves<QT>, QT == 1 ? 3 : 2) void tree_attn_pa
     const int end = piece.end - tree_blocks;
     const bool any_prefix = at < end;
     const int last = any_prefix ? at + (end - 1 - at) / KW * KW : 0;
-    PagedK keys{};
-    PagedV<D> v_this{}, v_next;
+    PagedK keys{}, k_other;
+    PagedV<D> v_this{}, v_other;
     Ids ids_next{};
     Block block{};
     unsigned vis_next = 0;
@@ -635,9 +642,12 @@ __global__ __launch_bounds__(64 * kWaves<QT>, QT == 1 ? 3 : 2) void tree_attn_pa
       auto visible = [&](int t) { return (unsigned)(tree_mask[t] >> t0) & there; };
       Scores<QT> s;
       float x[QT][8];
-      score_tree<QT, D>(s, kf, q_row);
-      hide<QT>(s, visible, p->c, g4);
-      settle<QT, D>(st, s, x, exponents<QT, D>(st, s, x, p->c), p->c);
+      auto score = [&](Scores<QT>& s) {
+        score_tree<QT, D>(s, kf, q_row);
+        hide<QT>(s, visible, p->c, g4);
+      };
+      score(s);
+      settle<QT, D>(st, x, exponents<QT, D>(st, s, x, p->c), p->c, score);
       weigh<QT>(x, pf);
       accumulate<QT, D>(st, pf, values);
       if (__builtin_expect(any_wild, 0)) {
@@ -682,27 +692,33 @@ __global__ __launch_bounds__(64 * kWaves<QT>, QT == 1 ? 3 : 2) void tree_attn_pa
       unsigned vis_this = 0;   // (no key is there)
       int third = min(at + KW, last);
       at -= KW;
-      for (;;) {
+      // (two turns stand in the loop, each with registers of its own for what it asks for: copied from one set to another, loads would be
+      // waited for in the turn that asks for them)
+      auto turn_of_stream = [&](PagedK& k_this, PagedK& k_third, PagedV<D>& v_this, PagedV<D>& v_next) {
         load_v(v_next, block);
         const unsigned vis = vis_next;
         block = place(third, ids_next);
         vis_next = vis_of(third, ids_next);
+        load_k(k_third, block);
         third = min(third + KW, last);
         ids_next = ids_of(third);
-        Scores<QT> s;
-        score_block<QT, D>(s, keys, q);
         weigh<QT>(x, pf);
-        load_k(keys, block);
+        __builtin_amdgcn_sched_barrier(0);
+        Scores<QT> s;
+        score_block<QT, D>(s, k_this, q);
         __builtin_amdgcn_sched_barrier(0);
         v_this.ready(vis_this, g4);
         accumulate<QT, D>(st, pf, v_this);
         if (__builtin_expect(vis != ~0u, 0)) hide<QT>(s, [&](int) { return vis; }, c, g4);
-        settle<QT, D>(st, s, x, exponents<QT, D>(st, s, x, c), c);
-        at += KW;
-        if (at > last) break;
-        v_this = v_next;
+        settle<QT, D>(st, x, exponents<QT, D>(st, s, x, c), c, [&](Scores<QT>& again) {
+          score_block<QT, D>(again, k_this, q);
+          if (vis != ~0u) hide<QT>(again, [&](int) { return vis; }, c, g4);
+        });
         vis_this = vis;
-      }
+        at += KW;
+        return at <= last;
+      };
+      while (turn_of_stream(keys, k_other, v_this, v_other) && turn_of_stream(k_other, keys, v_other, v_this)) {}
     }
   }
   p = fresh(p);
@@ -710,7 +726,7 @@ __global__ __launch_bounds__(64 * kWaves<QT>, QT == 1 ? 3 : 2) void tree_attn_pa
   // ---- the key-splitting wavefronts of a slab meet in LDS; each writes its share of the (row tile, four channel tiles) quads
 #pragma unroll
   for (int t = 0; t < QT; ++t) {
-    merge_ml[wave][t][lane] = make_float2(st.m[t], st.l[t][0]);
+    merge_ml[wave][t][lane] = make_float2(st.m[t], st.l[t]);
 #pragma unroll
     for (int e = 0; e < DT; ++e) merge_o[wave][t * DT + e][lane] = st.o[t][e];
   }

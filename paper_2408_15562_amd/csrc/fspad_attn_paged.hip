@@ -87,20 +87,16 @@ constexpr float kNoShift = -FLT_MAX;   // below every score: the first visible o
 struct SeqShape {
   int len, n, live, nb;
 };
-__device__ __forceinline__ SeqShape shape_of(Args p, int b) {
+__device__ __forceinline__ int2 seq_at(Args p, int b) { return b < p->B ? make_int2(p->kv_len[b], p->n_nodes[b]) : make_int2(0, 0); }
+__device__ __forceinline__ SeqShape shape_of(Args p, int2 seq) {
   SeqShape s;
-  s.len = b < p->B ? min(max(p->kv_len[b], 0), p->max_kv_len) : 0;
-  s.n = b < p->B ? min(max(p->n_nodes[b], 0), p->N) : 0;
+  s.len = min(max(seq.x, 0), p->max_kv_len);
+  s.n = min(max(seq.y, 0), p->N);
   s.live = (s.n * p->G + p->rows_per_group - 1) >> p->rows_shift;
   s.nb = s.live > 0 ? (s.len + kBlockKeys - 1) / kBlockKeys + (s.n + kBlockKeys - 1) / kBlockKeys : 0;
   return s;
 }
 
-__device__ __forceinline__ int wave_max(int x) {
-#pragma unroll
-  for (int off = 32; off > 0; off >>= 1) x = max(x, __shfl_xor(x, off));
-  return x;
-}
 __device__ __forceinline__ int last_lane(int x) { return __builtin_amdgcn_readlane(x, 63); }
 
 // Blocks of a piece, at most, for `blocks` blocks in `units` units of `longest` blocks at most. Pieces of one round (as many as the
@@ -124,78 +120,93 @@ __device__ __forceinline__ int piece_length(Args p, int blocks, int units, int l
   return max((int)len, p->least_blocks);
 }
 
-// This workgroup's piece. Pieces are numbered sequence by sequence, head by head, group by group, along the keys; workgroups eight
-// apart, which share a die and its L2 cache, take neighbouring ones.
+// How the call is cut, and the pieces of this workgroup. Pieces are numbered sequence by sequence, head by head, group by group, along the
+// keys; workgroups eight apart, which share a die and its L2 cache, take neighbouring ones.
 struct Piece {
-  int b, g, y, len, n, begin, end, nb, index, count;   // blocks [begin, end) of nb; index: its slot; count: pieces of the unit
-  bool any, dead;
+  int b, g, y, len, n, begin, end, index, count;   // blocks [begin, end) of a unit; index: its slot; count: pieces of the unit
+  bool dead;
 };
-__device__ __forceinline__ Piece piece_of(Args p, int w, int lane) {
-  SeqShape s = shape_of(p, lane);
-  int blocks = 0, units = 0, longest = 0;
-  for (int first = 0;;) {
-    blocks += last_lane(wave_sum_upto(p->Hkv * s.live * s.nb));
-    units += last_lane(wave_sum_upto(p->Hkv * s.live));
-    longest = max(longest, wave_max(s.nb));
-    first += 64;
-    if (first >= p->B) break;
-    s = shape_of(p, first + lane);
-  }
-  const int most = __builtin_amdgcn_readfirstlane(piece_length(p, blocks, units, longest));
-  // places of 64 sequences at a time
-  int places = 0, first = 0, upto, own, cuts;
-  auto count = [&] {
-    if (p->B > 64) s = shape_of(p, first + lane);
-    cuts = (s.nb + most - 1) / most;
-    own = first + lane < p->B ? p->Hkv * (s.live * cuts + p->groups - s.live) : 0;
-    upto = wave_sum_upto(own);
+struct Cutter {
+  Args p;
+  int lane, most, places;   // blocks of a piece, at most; pieces in all
+  int2 seq;                 // 64 sequences at a time, one a lane, from `first` on: length and nodes
+  int first, before, in_these;   // places before theirs, and theirs
+
+  struct Counts {
+    SeqShape s;
+    int cuts, own, upto;
   };
-  for (;;) {
-    count();
-    places += last_lane(upto);
-    first += 64;
-    if (first >= p->B) break;
+  __device__ __forceinline__ Counts count() const {
+    Counts c;
+    c.s = shape_of(p, seq);
+    c.cuts = (c.s.nb + most - 1) / most;
+    c.own = first + lane < p->B ? p->Hkv * (c.s.live * c.cuts + p->groups - c.s.live) : 0;
+    c.upto = wave_sum_upto(c.own);
+    return c;
   }
-  Piece r{};
-  const int share = (places + 7) >> 3, at = (w & 7) * share + (w >> 3);
-  r.any = (w >> 3) < share && at < places;
-  if (!r.any) return r;
-  int before = 0;
-  if (p->B > 64) {
-    for (first = 0;; first += 64) {
-      count();
-      if (at < before + last_lane(upto)) break;
-      before += last_lane(upto);
+  __device__ __forceinline__ Cutter(Args args, int lane_) : p(args), lane(lane_) {
+    seq = seq_at(p, lane);
+    int blocks = 0, units = 0, longest = 0;
+    for (first = 0;;) {
+      const SeqShape s = shape_of(p, seq);
+      const int of = p->Hkv * s.live;
+      blocks += last_lane(wave_sum_upto(of * s.nb));
+      units += last_lane(wave_sum_upto(of));
+      longest = max(longest, last_lane(wave_max_upto(s.nb)));
+      first += 64;
+      if (first >= p->B) break;
+      seq = seq_at(p, first + lane);
     }
-  } else {
-    first = 0;
+    most = __builtin_amdgcn_readfirstlane(piece_length(p, blocks, units, longest));
+    places = 0;
+    for (first = 0;; first += 64) {
+      if (p->B > 64) seq = seq_at(p, first + lane);
+      in_these = last_lane(count().upto);
+      places += in_these;
+      if (first + 64 >= p->B) break;
+    }
+    before = places - in_these;
   }
-  const int i = __builtin_ctzll(__ballot(at < before + upto));   // the sequence that the place lies in
-  r.b = first + i;
-  r.len = __builtin_amdgcn_readlane(s.len, i);
-  r.n = __builtin_amdgcn_readlane(s.n, i);
-  r.nb = __builtin_amdgcn_readlane(s.nb, i);
-  r.count = __builtin_amdgcn_readlane(cuts, i);
-  const int live = __builtin_amdgcn_readlane(s.live, i), rel = at - before - __builtin_amdgcn_readlane(upto - own, i);
-  r.index = at;
-  const int heads = p->Hkv * live * r.count;
-  r.dead = rel >= heads;
-  if (r.dead) {
-    const int others = p->groups - live, x = rel - heads;
-    r.g = x / others;
-    r.y = live + x - r.g * others;
-    r.count = 1;
-  } else {
-    const int u = rel / r.count, part = rel - u * r.count;
-    r.g = u / live;
-    r.y = u - r.g * live;
-    // equal pieces, the first ones a block longer
-    const int each = r.nb / r.count, more = r.nb - each * r.count;
-    r.begin = part * each + min(part, more);
-    r.end = r.begin + each + (part < more ? 1 : 0);
+  // place `at` < places
+  __device__ __forceinline__ Piece piece(int at) {
+    if (at < before || at >= before + in_these) {   // of other 64 sequences
+      before = in_these = 0;
+      first = -64;
+      do {
+        before += in_these;
+        first += 64;
+        seq = seq_at(p, first + lane);
+        in_these = last_lane(count().upto);
+      } while (at >= before + in_these);
+    }
+    const Counts c = count();
+    Piece r{};
+    const int i = __builtin_ctzll(__ballot(at < before + c.upto));   // the sequence that the place lies in
+    r.b = first + i;
+    r.len = __builtin_amdgcn_readlane(c.s.len, i);
+    r.n = __builtin_amdgcn_readlane(c.s.n, i);
+    r.count = __builtin_amdgcn_readlane(c.cuts, i);
+    r.index = at;
+    const int nb = __builtin_amdgcn_readlane(c.s.nb, i), live = __builtin_amdgcn_readlane(c.s.live, i);
+    const int rel = at - before - __builtin_amdgcn_readlane(c.upto - c.own, i), heads = p->Hkv * live * r.count;
+    r.dead = rel >= heads;
+    if (__builtin_expect(r.dead, 0)) {
+      const int others = p->groups - live, x = rel - heads;
+      r.g = x / others;
+      r.y = live + x - r.g * others;
+      r.count = 1;
+    } else {
+      const int u = rel / r.count, part = rel - u * r.count;
+      r.g = u / live;
+      r.y = u - r.g * live;
+      // equal pieces, the first ones a block longer
+      const int each = nb / r.count, more = nb - each * r.count;
+      r.begin = part * each + min(part, more);
+      r.end = r.begin + each + (part < more ? 1 : 0);
+    }
+    return r;
   }
-  return r;
-}
+};
 
 // -------------------------------------------------------------------------------------------- operands
 
@@ -470,10 +481,16 @@ __global__ __launch_bounds__(64 * kWaves<QT>, QT == 1 ? 3 : 2) void tree_attn_pa
   constexpr int KS = D / 32, DT = D / 16, ROWS = 16 * QT, WAVES = kWaves<QT>;
   __shared__ f32x4 merge_o[WAVES][QT * DT][64];
   __shared__ float2 merge_ml[WAVES][QT][64];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int col = lane & 15, g4 = lane >> 4;
-  const Piece piece = piece_of(p, blockIdx.x, lane);
-  if (!piece.any) return;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  Cutter cutter(p, threadIdx.x & 63);
+  // (the grid is a multiple of eight)
+  const int share = (cutter.places + 7) >> 3, die = blockIdx.x & 7, step = gridDim.x >> 3;
+  for (int nth = blockIdx.x >> 3; nth < share; nth += step) {
+  const int place_at = die * share + nth;
+  if (place_at >= cutter.places) break;
+  if (nth >= step) __syncthreads();   // the merge buffers are used again
+  const int lane = (int)here(threadIdx.x & 63), col = lane & 15, g4 = lane >> 4;   // (what is made of them is made for every piece)
+  const Piece piece = cutter.piece(place_at);
   const int b = piece.b, g = piece.g, y = piece.y, L = piece.len, n = piece.n;
   const int WS = 1 << p->ws_shift, KW = WAVES >> p->ws_shift;   // row slabs, wavefronts that split a slab's keys
   const int slab = wave & (WS - 1), kp = wave >> p->ws_shift;
@@ -775,6 +792,7 @@ __global__ __launch_bounds__(64 * kWaves<QT>, QT == 1 ? 3 : 2) void tree_attn_pa
         *reinterpret_cast<f32x4*>(part + quad_at<D>(tile, e0 / 4, i, lane)) = f32x4{o4[0][i], o4[1][i], o4[2][i], o4[3][i]};
     }
   }
+  }
 }
 
 // Joins the pieces of the units that were cut: out = sum_s 2^(m_s - M) O_s / sum_s 2^(m_s - M) l_s. A wavefront has one entry of a quad
@@ -836,8 +854,9 @@ __global__ __launch_bounds__(256) void tree_attn_paged_join_kernel(const PagedPa
 
 template <int D>
 void launch(const PagedPlan& pl, const PagedParams& p, hipStream_t stream) {
-  // (a multiple of eight: workgroup w takes place w / 8 of die w % 8's share)
-  const dim3 grid((unsigned)((pl.max_pieces + 7) / 8 * 8));
+  // a multiple of eight: workgroup w takes places w / 8, one grid's eighth further, .. of die w % 8's share
+  const int wgs = pl.max_pieces < pl.resident ? pl.max_pieces : pl.resident;
+  const dim3 grid((unsigned)((wgs + 7) / 8 * 8));
   if (pl.QT == 1) hipLaunchKernelGGL((tree_attn_paged_kernel<1, D>), grid, dim3(64 * kWaves<1>), 0, stream, p);
   else hipLaunchKernelGGL((tree_attn_paged_kernel<2, D>), grid, dim3(64 * kWaves<2>), 0, stream, p);
   if (!pl.may_cut) return;

@@ -40,7 +40,7 @@ inline PagedPlan plan_paged(const fspad_paged_desc& d) {
   const int key_waves = pl.QT == 1 ? 4 : 8 / pl.WS;
   pl.resident = pl.QT == 1 ? 3 * kPagedComputeUnits : kPagedComputeUnits;
   pl.least_blocks = 2 * key_waves;
-  pl.whole_blocks = 4 * key_waves;
+  pl.whole_blocks = 8 * key_waves;
   const int64_t units = (int64_t)d.batch * d.n_kv_heads * pl.groups, longest = paged_unit_blocks(d);
   pl.may_cut = d.workgroups > 0 || longest > pl.whole_blocks;
   // as many as there may be blocks, but at most two rounds of the device beside one for each unit

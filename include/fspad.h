@@ -380,7 +380,7 @@ fspad_status fspad_kv_commit(const fspad_attn_desc* desc, const void* k_tree, co
  *   K scales [D/32][P]
  *   V scales [D/32][P]
  * with the even channel of a byte in its low half: fspad_kv_page_bytes = Hkv * P * D * 17/16 in all. Pages start page_stride
- * bytes apart (a multiple of 16, at least the page's bytes: pools of several layers may be interleaved) in a pool of n_pages;
+ * bytes apart (a multiple of 16 below 2^32, at least the page's bytes: pools of several layers may be interleaved) in a pool of n_pages;
  * n_pages * page_tokens <= 2^31 - 1. Token t of page p is slot p * page_tokens + t.
  */
 typedef struct {
@@ -394,7 +394,7 @@ typedef struct {
   float softmax_scale;    /* 0 => 1/sqrt(D); finite, of any sign, else 2^-125 at least in magnitude (attention only) */
   int32_t page_tokens;    /* P: 16, 32, 64, 128 or 256 */
   int32_t n_pages;        /* pages of the pool, >= 1 */
-  int64_t page_stride;    /* bytes from page to page */
+  int64_t page_stride;    /* bytes from page to page, below 2^32 */
   int32_t table_width;    /* entries of a block table's row, >= 1 (attention only) */
   int32_t max_kv_len;     /* no sequence is longer, 0..table_width * P (attention only): the launch is laid out for it */
   int64_t table_stride;   /* entries from row to row of the block table, >= table_width (attention only) */

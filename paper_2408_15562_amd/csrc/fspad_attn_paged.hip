@@ -54,10 +54,11 @@ struct PagedParams {
   void* out;
   int2* cuts;       // per unit: first partial slot and number of pieces (0: the unit is complete in `out`)
   float* part;      // partial slots, one for every piece
-  int64_t page_stride, table_stride;
+  int64_t table_stride;
+  uint32_t page_stride;
   int32_t B, N, Hq, Hkv, G, page_shift, n_pages, max_kv_len;
   uint32_t g_rcp;   // reciprocal(G)
-  int32_t ws_shift, rows_shift, rows_per_group, groups, max_pieces, resident, least_blocks, whole_blocks, forced, out_bf16;
+  int32_t ws_shift, rows_shift, rows_per_group, groups, max_pieces, resident, least_blocks, whole_blocks, piece_cost, forced, out_bf16;
   float c;          // softmax scale * log2(e)
 };
 
@@ -101,21 +102,20 @@ __device__ __forceinline__ int last_lane(int x) { return __builtin_amdgcn_readla
 
 // Blocks of a piece, at most, for `blocks` blocks in `units` units of `longest` blocks at most. Pieces of one round (as many as the
 // device holds workgroups at once), if the units can be cut into so few, take as long as the longest of them; smaller ones in
-// several rounds share the device better and pay for starting and ending (kPieceCost blocks) more often.
-constexpr float kPieceCost = 12.0f;
+// several rounds share the device better and pay for starting and ending more often.
 __device__ __forceinline__ int piece_length(Args p, int blocks, int units, int longest) {
   const float slots = (float)(p->max_pieces - p->B * p->Hkv * p->groups);   // the sum of ceil(nb / len) is at most S / len + units
   if (p->forced > 0) return max((int)ceilf((float)blocks / slots) + 1, 1);
   if (longest <= p->whole_blocks) return max(longest, 1);
-  const float R = (float)p->resident, S = (float)blocks, U = (float)units;
-  float len = (float)longest, cost = S / R + fmaxf(U / R, 1.0f) * kPieceCost + 0.5f * len;   // whole units
+  const float R = (float)p->resident, S = (float)blocks, U = (float)units, piece_cost = (float)p->piece_cost;
+  float len = (float)longest, cost = S / R + fmaxf(U / R, 1.0f) * piece_cost + 0.5f * len;   // whole units
   if (units < p->resident) {
     const float one = fminf(ceilf(S / (R - U)), ceilf(len / floorf(R / U)));   // either way there are at most R pieces
     len = fminf(len, one);
-    cost = len + kPieceCost;
+    cost = len + piece_cost;
   }
-  const float many = ceilf(__builtin_sqrtf(2.0f * kPieceCost * S / R));
-  if ((S + (S / many + 0.5f * U) * kPieceCost) / R + 0.5f * many < cost) len = fminf(len, many);
+  const float many = ceilf(__builtin_sqrtf(2.0f * piece_cost * S / R));
+  if ((S + (S / many + 0.5f * U) * piece_cost) / R + 0.5f * many < cost) len = fminf(len, many);
   len = fmaxf(len, ceilf(S / slots) + 1.0f);
   return max((int)len, p->least_blocks);
 }
@@ -311,7 +311,10 @@ struct PagedV {
 
   __device__ __forceinline__ void ready(unsigned vis, int g4) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) f[j] = __builtin_bit_cast(float, ((scale[j >> 2] >> (8 * (j & 3))) & 0xffu) << 23);
+    for (int j = 0; j < 8; ++j) {   // (the conversion takes the exponent of its scale: what lies around the byte does not matter)
+      const unsigned w = scale[j >> 2];
+      f[j] = __builtin_bit_cast(float, (j & 3) == 3 ? w >> 1 : w << (23 - 8 * (j & 3)));
+    }
     if (__builtin_expect(vis != ~0u, 0)) {
       const unsigned own = vis >> here(4 * g4);
 #pragma unroll
@@ -472,13 +475,11 @@ __device__ __forceinline__ int64_t slot_floats(int rows) { return (int64_t)rows 
 template <int D>
 __device__ __forceinline__ int quad_at(int tile, int quad, int entry, int lane) { return (((tile * (D / 64) + quad) * 4 + entry) * 64 + lane) * 4; }
 
-template <int QT>
-constexpr int kWaves = QT == 1 ? 4 : 8;
-
-template <int QT, int D>
-__global__ __launch_bounds__(64 * kWaves<QT>, QT == 1 ? 3 : 2) void tree_attn_paged_kernel(const PagedParams) {
+// WIDE: a page holds a block's 32 keys (pages of 16 keys: a block's halves lie on two).
+template <int QT, int D, bool WIDE>
+__global__ __launch_bounds__(64 * paged_waves(QT, D), paged_waves(QT, D) * paged_resident(QT, D) / 4) void tree_attn_paged_kernel(const PagedParams) {
   Args p = (Args)__builtin_amdgcn_kernarg_segment_ptr();
-  constexpr int KS = D / 32, DT = D / 16, ROWS = 16 * QT, WAVES = kWaves<QT>;
+  constexpr int KS = D / 32, DT = D / 16, ROWS = 16 * QT, WAVES = paged_waves(QT, D);
   __shared__ f32x4 merge_o[WAVES][QT * DT][64];
   __shared__ float2 merge_ml[WAVES][QT][64];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -529,53 +530,61 @@ __global__ __launch_bounds__(64 * kWaves<QT>, QT == 1 ? 3 : 2) void tree_attn_pa
     const unsigned vs_off = (unsigned)(2 * codes + scales + (col * (D / 16) / 32) * P + 4 * g4);
     GlobalBytes const pool = (GlobalBytes)p->pages + (int64_t)g * page_head_bytes(D, P);
     ScalarI32 const table = (ScalarI32)p->table + (int64_t)b * p->table_stride;
-    const int64_t page_stride = p->page_stride;
+    const uint32_t page_stride = p->page_stride;
     const int page_shift = p->page_shift, n_pages = p->n_pages;
-    struct Ids { int id[2]; };   // pages of the two half blocks
+    constexpr int HALVES = WIDE ? 1 : 2, KEYS = 32 / HALVES;
+    struct Ids { int id[HALVES]; };
     auto ids_of = [&](int at) {   // (places of the prefix: block `at` has keys 32 at ..)
-      const int t0 = at * kBlockKeys;
-      return Ids{{table[t0 >> page_shift], table[min(t0 + 16, L - 1) >> page_shift]}};
+      const unsigned t0 = (unsigned)at * kBlockKeys;
+      Ids r;
+      r.id[0] = table[t0 >> page_shift];
+      if constexpr (!WIDE) r.id[1] = table[min(t0 + 16, (unsigned)L - 1) >> page_shift];
+      return r;
     };
-    auto vis_of = [&](int at, const Ids& ids) {   // bit t: key t is there
-      const int left = L - at * kBlockKeys;
-      unsigned vis = left >= kBlockKeys ? ~0u : left > 0 ? (1u << left) - 1u : 0u;
-      if ((unsigned)ids.id[0] >= (unsigned)n_pages) vis &= 0xffff0000u;
-      if ((unsigned)ids.id[1] >= (unsigned)n_pages) vis &= 0x0000ffffu;
+    auto vis_of = [&](int at, const Ids& ids) {   // bit t: key t is there; block `at` has one at least
+      unsigned vis = ~0u >> (32 - min(L - at * kBlockKeys, 32));
+#pragma unroll
+      for (int half = 0; half < HALVES; ++half)
+        if ((unsigned)ids.id[half] >= (unsigned)n_pages) vis &= WIDE ? 0u : half == 0 ? 0xffff0000u : 0x0000ffffu;
       return vis;
     };
-    struct Block { GlobalBytes code[2], scale[2]; };
+    struct Block { GlobalBytes code[HALVES], scale[HALVES]; };
     auto place = [&](int at, const Ids& ids) {
       Block r;
 #pragma unroll
-      for (int half = 0; half < 2; ++half) {
-        const int id = (unsigned)ids.id[half] < (unsigned)n_pages ? ids.id[half] : 0, in_page = (at * kBlockKeys + 16 * half) & (P - 1);
-        GlobalBytes const page = pool + (int64_t)id * page_stride;
+      for (int half = 0; half < HALVES; ++half) {
+        const unsigned id = (unsigned)ids.id[half] < (unsigned)n_pages ? (unsigned)ids.id[half] : 0u;
+        const unsigned in_page = ((unsigned)at * kBlockKeys + 16u * half) & (unsigned)(P - 1);
+        GlobalBytes const page = pool + (uint64_t)id * page_stride;
         r.code[half] = page + in_page * (D / 2);
         r.scale[half] = page + in_page;
       }
       return r;
     };
+    // (the second 16 keys of a wide block are 16 rows further on)
     auto load_k = [&](PagedK& x, const Block& block) {
       const unsigned k_at = here(k_off), ks_at = here(ks_off);
 #pragma unroll
       for (int kt = 0; kt < 2; ++kt) {
-        x.c[kt] = *(const __attribute__((address_space(1))) u32x4*)(block.code[kt] + k_at);
-        x.scale[kt] = ((const __attribute__((address_space(1))) Unaligned*)(block.scale[kt] + ks_at))->word;   // (the products take its first byte)
+        const int half = WIDE ? 0 : kt, further = WIDE ? 16 * kt : 0;
+        x.c[kt] = *(const __attribute__((address_space(1))) u32x4*)(block.code[half] + k_at + further * (D / 2));
+        x.scale[kt] = ((const __attribute__((address_space(1))) Unaligned*)(block.scale[half] + ks_at + further))->word;   // (the products take its first byte)
       }
     };
     auto load_v = [&](PagedV<D>& x, const Block& block) {
       const unsigned v_at = here(v_off), vs_at = here(vs_off);
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
+        const int half = WIDE ? 0 : h, further = WIDE ? 16 * h : 0;
         if constexpr (D == 128) {
-          const u32x4 w = *(const __attribute__((address_space(1))) u32x4*)(block.code[h] + v_at);
+          const u32x4 w = *(const __attribute__((address_space(1))) u32x4*)(block.code[half] + v_at + further * (D / 2));
 #pragma unroll
           for (int i = 0; i < 4; ++i) x.c[4 * h + i] = w[i];
         } else {
-          const u32x2 w = *(const __attribute__((address_space(1))) u32x2*)(block.code[h] + v_at);
+          const u32x2 w = *(const __attribute__((address_space(1))) u32x2*)(block.code[half] + v_at + further * (D / 2));
           x.c[2 * h] = w[0]; x.c[2 * h + 1] = w[1];
         }
-        x.scale[h] = *(const __attribute__((address_space(1))) unsigned*)(block.scale[h] + vs_at);
+        x.scale[h] = *(const __attribute__((address_space(1))) unsigned*)(block.scale[half] + vs_at + further);
       }
     };
 
@@ -852,13 +861,14 @@ __global__ __launch_bounds__(256) void tree_attn_paged_join_kernel(const PagedPa
   }
 }
 
-template <int D>
+template <int D, bool WIDE>
 void launch(const PagedPlan& pl, const PagedParams& p, hipStream_t stream) {
   // a multiple of eight: workgroup w takes places w / 8, one grid's eighth further, .. of die w % 8's share
   const int wgs = pl.max_pieces < pl.resident ? pl.max_pieces : pl.resident;
   const dim3 grid((unsigned)((wgs + 7) / 8 * 8));
-  if (pl.QT == 1) hipLaunchKernelGGL((tree_attn_paged_kernel<1, D>), grid, dim3(64 * kWaves<1>), 0, stream, p);
-  else hipLaunchKernelGGL((tree_attn_paged_kernel<2, D>), grid, dim3(64 * kWaves<2>), 0, stream, p);
+  if (pl.QT == 1) hipLaunchKernelGGL((tree_attn_paged_kernel<1, D, WIDE>), grid, dim3(64 * paged_waves(1, D)), 0, stream, p);
+  else if (pl.QT == 2) hipLaunchKernelGGL((tree_attn_paged_kernel<2, D, WIDE>), grid, dim3(64 * paged_waves(2, D)), 0, stream, p);
+  else if constexpr (D == 64) hipLaunchKernelGGL((tree_attn_paged_kernel<4, D, WIDE>), grid, dim3(64 * paged_waves(4, D)), 0, stream, p);
   if (!pl.may_cut) return;
   const int rows = pl.rows_per_group < p.N * p.G ? pl.rows_per_group : p.N * p.G;
   hipLaunchKernelGGL((tree_attn_paged_join_kernel<D>), dim3((unsigned)((rows + 15) / 16 * (D / 64)), (unsigned)p.Hkv, (unsigned)(p.B * pl.groups)),
@@ -890,16 +900,17 @@ extern "C" fspad_status fspad_tree_attn_paged(const fspad_paged_desc* desc, cons
   p.pages = static_cast<const char*>(pages); p.table = block_table; p.kv_len = kv_len; p.n_nodes = n_nodes; p.mask = anc_mask;
   p.out = out; p.cuts = static_cast<int2*>(workspace);
   p.part = reinterpret_cast<float*>(static_cast<char*>(workspace) + pl.cuts_bytes);
-  p.page_stride = d.page_stride; p.table_stride = d.table_stride;
+  p.page_stride = (uint32_t)d.page_stride; p.table_stride = d.table_stride;
   p.B = d.batch; p.N = d.n_nodes_max; p.Hq = d.n_q_heads; p.Hkv = d.n_kv_heads; p.G = d.n_q_heads / d.n_kv_heads;
   p.page_shift = log2_of(d.page_tokens); p.n_pages = d.n_pages; p.max_kv_len = d.max_kv_len;
   p.g_rcp = reciprocal(p.G);
   p.ws_shift = log2_of(pl.WS); p.rows_shift = log2_of(pl.rows_per_group); p.rows_per_group = pl.rows_per_group; p.groups = pl.groups;
-  p.max_pieces = pl.max_pieces; p.resident = pl.resident; p.least_blocks = pl.least_blocks; p.whole_blocks = pl.whole_blocks; p.forced = d.workgroups;
+  p.max_pieces = pl.max_pieces; p.resident = pl.resident; p.least_blocks = pl.least_blocks; p.whole_blocks = pl.whole_blocks; p.piece_cost = pl.piece_cost; p.forced = d.workgroups;
   p.out_bf16 = d.out_dtype == FSPAD_BF16;
   p.c = c;
   hipStream_t stream = reinterpret_cast<hipStream_t>(hip_stream);
-  if (d.head_dim == 128) launch<128>(pl, p, stream);
-  else launch<64>(pl, p, stream);
+  const bool wide = d.page_tokens >= kBlockKeys;
+  if (d.head_dim == 128) wide ? launch<128, true>(pl, p, stream) : launch<128, false>(pl, p, stream);
+  else wide ? launch<64, true>(pl, p, stream) : launch<64, false>(pl, p, stream);
   return hipGetLastError() == hipSuccess ? FSPAD_OK : FSPAD_ERR_HIP;
 }

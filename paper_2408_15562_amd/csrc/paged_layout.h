@@ -24,7 +24,7 @@ inline fspad_status check_pool(const fspad_paged_desc& d) {
   if (d.n_kv_heads < 1 || (d.head_dim != 64 && d.head_dim != 128) || !page_tokens_ok(d.page_tokens)) return FSPAD_ERR_SHAPE;
   if (d.io_dtype != FSPAD_BF16) return FSPAD_ERR_DTYPE;
   const int64_t page_bytes = (int64_t)d.n_kv_heads * page_head_bytes(d.head_dim, d.page_tokens);
-  if (page_bytes > INT32_MAX || d.page_stride < page_bytes || d.page_stride % 16 != 0) return FSPAD_ERR_SHAPE;
+  if (page_bytes > INT32_MAX || d.page_stride < page_bytes || d.page_stride % 16 != 0 || d.page_stride > UINT32_MAX) return FSPAD_ERR_SHAPE;
   if (d.n_pages < 1 || (int64_t)d.n_pages * d.page_tokens > INT32_MAX) return FSPAD_ERR_SHAPE;   // slots are 32-bit
   return FSPAD_OK;
 }

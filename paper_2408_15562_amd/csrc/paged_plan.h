@@ -14,12 +14,16 @@ constexpr int kBlockKeys = 32;
 constexpr int kPagedMaxBatch = 1024;
 constexpr int kPagedComputeUnits = 256;
 
+constexpr int paged_waves(int QT, int D) { return QT == 2 || (QT == 4 && D == 64) ? 8 : 4; }
+constexpr int paged_resident(int QT, int D) { return QT == 1 ? (D == 64 ? 4 : 3) : 1; }   // workgroups of a compute unit
+
 struct PagedPlan {
   int QT, WS;            // 16-row tiles of a wavefront, row slabs of a workgroup (its other wavefronts split a slab's keys)
   int rows_per_group;    // WS * 16 * QT: 16, 32 or 64
   int groups;            // row groups of a kv head's N * G rows
   int resident;          // workgroups that the device holds at once
   int least_blocks, whole_blocks;   // no piece is shorter, no unit of up to so many blocks is cut
+  int piece_cost;        // what starting and ending a piece takes, in blocks
   bool may_cut;          // a unit can be so long that it is cut
   int max_pieces;
   size_t cuts_bytes, workspace_bytes;
@@ -35,12 +39,13 @@ inline PagedPlan plan_paged(const fspad_paged_desc& d) {
   const int rows = d.n_nodes_max * (d.n_q_heads / d.n_kv_heads);
   pl.rows_per_group = rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
   pl.groups = (rows + pl.rows_per_group - 1) / pl.rows_per_group;
-  pl.QT = pl.rows_per_group == 16 ? 1 : 2;
-  pl.WS = pl.rows_per_group == 64 ? 2 : 1;
-  const int key_waves = pl.QT == 1 ? 4 : 8 / pl.WS;
-  pl.resident = pl.QT == 1 ? 3 * kPagedComputeUnits : kPagedComputeUnits;
+  pl.QT = pl.rows_per_group == 64 && d.head_dim == 128 ? 2 : pl.rows_per_group / 16;
+  pl.WS = pl.rows_per_group / (16 * pl.QT);
+  const int key_waves = paged_waves(pl.QT, d.head_dim) / pl.WS;
+  pl.resident = paged_resident(pl.QT, d.head_dim) * kPagedComputeUnits;
   pl.least_blocks = 2 * key_waves;
   pl.whole_blocks = 8 * key_waves;
+  pl.piece_cost = 10 * key_waves;
   const int64_t units = (int64_t)d.batch * d.n_kv_heads * pl.groups, longest = paged_unit_blocks(d);
   pl.may_cut = d.workgroups > 0 || longest > pl.whole_blocks;
   // as many as there may be blocks, but at most two rounds of the device beside one for each unit

@@ -34,7 +34,7 @@ def test_page_bytes(hkv, D, P, want):
 
 
 @pytest.mark.parametrize("change", [dict(n_kv_heads=0), dict(head_dim=96), dict(page_tokens=24), dict(page_tokens=8), dict(n_pages=0),
-                                    dict(page_stride=2 * 2176 - 16), dict(page_stride=2 * 2176 + 8), dict(n_pages=1 << 27), dict(n_kv_heads=65536),
+                                    dict(page_stride=2 * 2176 - 16), dict(page_stride=2 * 2176 + 8), dict(page_stride=1 << 32), dict(n_pages=1 << 27), dict(n_kv_heads=65536),
                                     dict(n_kv_heads=1 << 30)])
 def test_store_and_load_refuse_shapes(lib, change):
     d = _desc(**change)

@@ -204,6 +204,11 @@ struct Cutter {
       r.begin = part * each + min(part, more);
       r.end = r.begin + each + (part < more ? 1 : 0);
     }
+    // (quotients come from the vector unit: what follows is the same in all lanes)
+    r.g = __builtin_amdgcn_readfirstlane(r.g);
+    r.y = __builtin_amdgcn_readfirstlane(r.y);
+    r.begin = __builtin_amdgcn_readfirstlane(r.begin);
+    r.end = __builtin_amdgcn_readfirstlane(r.end);
     return r;
   }
 };
@@ -735,8 +740,14 @@ __global__ __launch_bounds__(64 * paged_waves(QT, D), paged_waves(QT, D) * paged
         __builtin_amdgcn_sched_barrier(0);
         v_this.ready(vis_this, g4);
         accumulate<QT, D>(st, pf, v_this);
-        if (__builtin_expect(vis != ~0u, 0)) hide<QT>(s, [&](int) { return vis; }, c, g4);
-        settle<QT, D>(st, x, exponents<QT, D>(st, s, x, c), c, [&](Scores<QT>& again) {
+        float most;
+        if (__builtin_expect(vis != ~0u, 0)) {
+          hide<QT>(s, [&](int) { return vis; }, c, g4);
+          most = exponents<QT, D>(st, s, x, c);
+        } else {
+          most = exponents<QT, D>(st, s, x, c);
+        }
+        settle<QT, D>(st, x, most, c, [&](Scores<QT>& again) {
           score_block<QT, D>(again, k_this, q);
           if (vis != ~0u) hide<QT>(again, [&](int) { return vis; }, c, g4);
         });

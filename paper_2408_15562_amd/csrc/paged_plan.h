@@ -14,17 +14,18 @@ constexpr int kBlockKeys = 32;
 constexpr int kPagedMaxBatch = 1024;
 constexpr int kPagedComputeUnits = 256;
 
-constexpr int paged_waves(int QT, int D) { return QT == 2 || (QT == 4 && D == 64) ? 8 : 4; }
-constexpr int paged_resident(int QT, int D) { return QT == 1 ? (D == 64 ? 4 : 3) : 1; }   // workgroups of a compute unit
+constexpr int paged_waves(int rows_per_wave) { return rows_per_wave == 16 ? 4 : 8; }
+constexpr int paged_resident(int rows_per_wave, int D) { return rows_per_wave == 16 ? (D == 64 ? 4 : 3) : 1; }   // workgroups of a compute unit
 
 struct PagedPlan {
-  int QT, WS;            // 16-row tiles of a wavefront, row slabs of a workgroup (its other wavefronts split a slab's keys)
-  int rows_per_group;    // WS * 16 * QT: 16, 32 or 64
+  int rows_per_wave, WS; // row slabs of a workgroup (its other wavefronts split a slab's keys)
+  int rows_per_group;    // WS * rows_per_wave: 16, 32 or 64
   int groups;            // row groups of a kv head's N * G rows
   int resident;          // workgroups that the device holds at once
   int least_blocks, whole_blocks;   // no piece is shorter, no unit of up to so many blocks is cut
-  int piece_cost;        // what starting and ending a piece takes, in blocks
+  int piece_cost, join_cost, dead_cost;   // what starting and ending a piece takes, joining pieces, a unit without nodes, in blocks
   bool may_cut;          // a unit can be so long that it is cut
+  bool lines;            // workgroups may take windows of all units: two slots each
   int max_pieces;
   size_t cuts_bytes, workspace_bytes;
 };
@@ -33,25 +34,29 @@ inline int64_t paged_unit_blocks(const fspad_paged_desc& d) {   // at most
   return ((int64_t)d.max_kv_len + kBlockKeys - 1) / kBlockKeys + (d.n_nodes_max + kBlockKeys - 1) / kBlockKeys;
 }
 
-// Rows of a workgroup: 16 (four wavefronts), 32 or 64 (eight), the number that leaves the fewest of them empty.
+// Rows of a workgroup: 16 (four wavefronts), 32 or 64 (eight), the number that leaves the fewest of them empty. A piece starts and ends in 8 us, pieces
+// are joined in 5 us, and a wavefront takes 0.3 us a block when the device is full: the costs below.
 inline PagedPlan plan_paged(const fspad_paged_desc& d) {
   PagedPlan pl{};
   const int rows = d.n_nodes_max * (d.n_q_heads / d.n_kv_heads);
   pl.rows_per_group = rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
   pl.groups = (rows + pl.rows_per_group - 1) / pl.rows_per_group;
-  pl.QT = pl.rows_per_group == 64 && d.head_dim == 128 ? 2 : pl.rows_per_group / 16;
-  pl.WS = pl.rows_per_group / (16 * pl.QT);
-  const int key_waves = paged_waves(pl.QT, d.head_dim) / pl.WS;
-  pl.resident = paged_resident(pl.QT, d.head_dim) * kPagedComputeUnits;
+  pl.rows_per_wave = pl.rows_per_group == 64 && d.head_dim == 128 ? 32 : pl.rows_per_group;
+  pl.WS = pl.rows_per_group / pl.rows_per_wave;
+  const int key_waves = paged_waves(pl.rows_per_wave) / pl.WS;
+  pl.resident = paged_resident(pl.rows_per_wave, d.head_dim) * kPagedComputeUnits;
   pl.least_blocks = 2 * key_waves;
   pl.whole_blocks = 8 * key_waves;
-  pl.piece_cost = 10 * key_waves;
+  pl.piece_cost = 8 * key_waves;
+  pl.join_cost = 4 * key_waves;
+  pl.dead_cost = key_waves;
   const int64_t units = (int64_t)d.batch * d.n_kv_heads * pl.groups, longest = paged_unit_blocks(d);
   pl.may_cut = d.workgroups > 0 || longest > pl.whole_blocks;
   // as many as there may be blocks, but at most two rounds of the device beside one for each unit
   int64_t cut = d.workgroups > 0 ? d.workgroups : 2 * pl.resident;
   if (cut > units * longest) cut = units * longest;
   pl.max_pieces = (int)(units + (pl.may_cut ? cut : 0));
+  pl.lines = pl.rows_per_wave > 16 && pl.max_pieces >= 2 * pl.resident;
   pl.cuts_bytes = (size_t)((units * 8 + 15) / 16 * 16);
   pl.workspace_bytes = pl.cuts_bytes + (pl.may_cut ? (size_t)pl.max_pieces * pl.rows_per_group * (d.head_dim + 2) * 4 : 0);
   return pl;

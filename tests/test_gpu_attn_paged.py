@@ -232,3 +232,21 @@ def test_long_prefix_single_token():
     c = Case(15, 1, 1, 8, 1, 128, 256, [40000])
     c.check()
     c.check(workgroups=1)
+
+
+@pytest.mark.parametrize("B,N,Hq,Hkv,D,P,top", [(24, 64, 16, 8, 128, 64, 1500), (24, 40, 16, 8, 128, 16, 1300), (20, 64, 32, 8, 64, 32, 2300), (70, 33, 8, 4, 128, 32, 1100),
+                                                (17, 32, 16, 8, 128, 128, 4100)])
+def test_more_units_than_workgroups(B, N, Hq, Hkv, D, P, top):
+    """Row groups of all heads and sequences in equal windows: units that start and end in any place of one, whole ones, ones without
+    nodes, last groups of a few rows. Twice the same bits."""
+    rng = np.random.default_rng(B + top)
+    kv_len, nodes = rng.integers(0, top // 2, B), rng.integers(1, N + 1, B)
+    kv_len[:3], kv_len[3:6] = top, [0, 1, 33]
+    nodes[:2], nodes[-2:] = N, [0, 1]
+    if B == 17:
+        kv_len[:], nodes[:] = top - np.arange(B), N
+    c = Case(B, B, N, Hq, Hkv, D, P, kv_len, nodes)
+    got = c.check()
+    for b in range(B):
+        assert np.all(got[b, nodes[b]:] == 0)
+    assert torch.equal(c.run(), c.run(poison=False))

@@ -20,7 +20,9 @@ typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
 // Store and load. Pure data movement with a conversion: 4 bytes of bf16 K and V a channel against 17/16 of the pages, so what
 // bounds a large call is memory. A lane holds 8 channels of one row (16 bytes of bf16, 4 of codes), 16 lanes a row of D = 128
 // (8 of D = 64), four lanes a block. A wavefront takes neighbouring rows of ONE head: a prompt's rows are neighbours in their
-// page too, so that a store instruction writes whole 256-byte stretches of codes.
+// page too, so that a store instruction writes whole 256-byte stretches of codes. Workgroups that run at the same time have all heads of
+// neighbouring rows, whose bf16 lies in a row: 8191 rows of 32 heads, D = 128 (170 MB), are stored in 33 us and loaded in 35 us, 5.1 and
+// 4.9 TB/s (39 and 40 us head after head, which reads 256 bytes in every 8 KB); 16384 rows of 8 heads are loaded in 15 us (5.6 TB/s).
 struct RowsParams {
   char* k;               // [rows] x [Hkv] x D bf16: read by the store, written by the load
   char* v;
@@ -98,50 +100,50 @@ __device__ __forceinline__ u32x4 decode8(unsigned c, unsigned s) {
 template <int D>
 __global__ __launch_bounds__(kRowThreads) void kv_store_paged_kernel(const RowsParams p) {
   constexpr int LPR = D / 8, RPW = kRowThreads / LPR;   // lanes of a row, rows of a workgroup
-  const int head = blockIdx.y, part = threadIdx.x % LPR;
-  const int row = blockIdx.x * RPW + threadIdx.x / LPR;
-  if (row >= p.rows) return;                            // (whole rows: a block's four lanes stay together)
-  const int slot = p.slots[row];
-  if ((unsigned)slot >= (unsigned)p.n_slots) return;
-  const int64_t at = row * p.row_stride + head * p.head_stride + part * 16;
-  const u32x4 kx = *reinterpret_cast<const u32x4*>(p.k + at);
-  const u32x4 vx = *reinterpret_cast<const u32x4*>(p.v + at);
-  const unsigned ks = block_scale(block_top(kx)), vs = block_scale(block_top(vx));
-  const unsigned kc = encode8(kx, ks), vc = encode8(vx, vs);
-  const SlotAddr a = slot_addr<D>(p, slot, head, part);
-  *reinterpret_cast<unsigned*>(a.k_code) = kc;
-  if constexpr (D == 128) {
-    *reinterpret_cast<unsigned*>(a.v_code) = vc;
-  } else {   // two runs of four channels, 16 bytes apart
-    *reinterpret_cast<unsigned short*>(a.v_code) = (unsigned short)vc;
-    *reinterpret_cast<unsigned short*>(a.v_code + 16) = (unsigned short)(vc >> 16);
-  }
-  if (part % 4 == 0) {
-    *a.k_scale = (char)ks;
-    *a.v_scale = (char)vs;
+  const int head = blockIdx.x, part = threadIdx.x % LPR;
+  for (int64_t row = (int64_t)blockIdx.y * RPW + threadIdx.x / LPR; row < p.rows; row += (int64_t)gridDim.y * RPW) {   // (whole rows: a block's four lanes stay together)
+    const int slot = p.slots[row];
+    if ((unsigned)slot >= (unsigned)p.n_slots) continue;
+    const int64_t at = row * p.row_stride + head * p.head_stride + part * 16;
+    const u32x4 kx = *reinterpret_cast<const u32x4*>(p.k + at);
+    const u32x4 vx = *reinterpret_cast<const u32x4*>(p.v + at);
+    const unsigned ks = block_scale(block_top(kx)), vs = block_scale(block_top(vx));
+    const unsigned kc = encode8(kx, ks), vc = encode8(vx, vs);
+    const SlotAddr a = slot_addr<D>(p, slot, head, part);
+    *reinterpret_cast<unsigned*>(a.k_code) = kc;
+    if constexpr (D == 128) {
+      *reinterpret_cast<unsigned*>(a.v_code) = vc;
+    } else {   // two runs of four channels, 16 bytes apart
+      *reinterpret_cast<unsigned short*>(a.v_code) = (unsigned short)vc;
+      *reinterpret_cast<unsigned short*>(a.v_code + 16) = (unsigned short)(vc >> 16);
+    }
+    if (part % 4 == 0) {
+      *a.k_scale = (char)ks;
+      *a.v_scale = (char)vs;
+    }
   }
 }
 
 template <int D>
 __global__ __launch_bounds__(kRowThreads) void kv_load_paged_kernel(const RowsParams p) {
   constexpr int LPR = D / 8, RPW = kRowThreads / LPR;
-  const int head = blockIdx.y, part = threadIdx.x % LPR;
-  const int row = blockIdx.x * RPW + threadIdx.x / LPR;
-  if (row >= p.rows) return;
-  const int slot = p.slots[row];
-  u32x4 kx = {0u, 0u, 0u, 0u}, vx = {0u, 0u, 0u, 0u};
-  if ((unsigned)slot < (unsigned)p.n_slots) {
-    const SlotAddr a = slot_addr<D>(p, slot, head, part);
-    const unsigned kc = *reinterpret_cast<const unsigned*>(a.k_code);
-    unsigned vc;
-    if constexpr (D == 128) vc = *reinterpret_cast<const unsigned*>(a.v_code);
-    else vc = *reinterpret_cast<const unsigned short*>(a.v_code) | ((unsigned)*reinterpret_cast<const unsigned short*>(a.v_code + 16) << 16);
-    kx = decode8(kc, (unsigned char)*a.k_scale);
-    vx = decode8(vc, (unsigned char)*a.v_scale);
+  const int head = blockIdx.x, part = threadIdx.x % LPR;
+  for (int64_t row = (int64_t)blockIdx.y * RPW + threadIdx.x / LPR; row < p.rows; row += (int64_t)gridDim.y * RPW) {
+    const int slot = p.slots[row];
+    u32x4 kx = {0u, 0u, 0u, 0u}, vx = {0u, 0u, 0u, 0u};
+    if ((unsigned)slot < (unsigned)p.n_slots) {
+      const SlotAddr a = slot_addr<D>(p, slot, head, part);
+      const unsigned kc = *reinterpret_cast<const unsigned*>(a.k_code);
+      unsigned vc;
+      if constexpr (D == 128) vc = *reinterpret_cast<const unsigned*>(a.v_code);
+      else vc = *reinterpret_cast<const unsigned short*>(a.v_code) | ((unsigned)*reinterpret_cast<const unsigned short*>(a.v_code + 16) << 16);
+      kx = decode8(kc, (unsigned char)*a.k_scale);
+      vx = decode8(vc, (unsigned char)*a.v_scale);
+    }
+    const int64_t at = row * p.row_stride + head * p.head_stride + part * 16;
+    *reinterpret_cast<u32x4*>(p.k + at) = kx;
+    *reinterpret_cast<u32x4*>(p.v + at) = vx;
   }
-  const int64_t at = row * p.row_stride + head * p.head_stride + part * 16;
-  *reinterpret_cast<u32x4*>(p.k + at) = kx;
-  *reinterpret_cast<u32x4*>(p.v + at) = vx;
 }
 
 fspad_status move_rows(bool store, const fspad_paged_desc* desc, int32_t rows, void* k, void* v, int64_t row_stride,
@@ -161,7 +163,8 @@ fspad_status move_rows(bool store, const fspad_paged_desc* desc, int32_t rows, v
   p.row_stride = row_stride * 2; p.head_stride = head_stride * 2; p.page_stride = d.page_stride;
   p.rows = rows; p.n_slots = d.n_pages * d.page_tokens; p.page_shift = log2_of(d.page_tokens); p.D = d.head_dim;
   const int rpw = kRowThreads / (d.head_dim / 8);
-  const dim3 grid((unsigned)((rows + (int64_t)rpw - 1) / rpw), (unsigned)d.n_kv_heads);
+  const int64_t wgs = (rows + (int64_t)rpw - 1) / rpw;
+  const dim3 grid((unsigned)d.n_kv_heads, (unsigned)(wgs < 65535 ? wgs : 65535));
   hipStream_t stream = reinterpret_cast<hipStream_t>(hip_stream);
   if (store) {
     if (d.head_dim == 128) hipLaunchKernelGGL(kv_store_paged_kernel<128>, grid, dim3(kRowThreads), 0, stream, p);

@@ -45,8 +45,10 @@ inline PagedPlan plan_paged(const fspad_paged_desc& d) {
   pl.WS = pl.rows_per_group / pl.rows_per_wave;
   const int key_waves = paged_waves(pl.rows_per_wave) / pl.WS;
   pl.resident = paged_resident(pl.rows_per_wave, d.head_dim) * kPagedComputeUnits;
+  // Joining costs as much as 55 blocks of 16 rows, 30 of 32 and more. One token, 8 kv heads, D = 128: 1024 tokens whole 10.9 us, cut
+  // 12.7; 2048 14.1 and 14.5; 4096 20.2 and 17.5. 26 nodes on 32 heads: 1500 tokens 17.5 whole; 2048 19.6 and 19.4; 3000 22.8 and 19.8.
   pl.least_blocks = 2 * key_waves;
-  pl.whole_blocks = 8 * key_waves;
+  pl.whole_blocks = (pl.rows_per_wave == 16 ? 18 : 9) * key_waves;
   pl.piece_cost = 8 * key_waves;
   pl.join_cost = 4 * key_waves;
   pl.dead_cost = key_waves;

@@ -401,13 +401,19 @@ struct Places {
 };
 
 // WIDE: a page holds a block's 32 keys (pages of 16 keys: a block's halves lie on two).
-template <class Form, bool WIDE>
-__global__ __launch_bounds__(64 * paged_waves(Form::ROWS), paged_waves(Form::ROWS) * paged_resident(Form::ROWS, Form::HEAD_DIM) / 4)
+template <class Form, int WAVES, bool WIDE>
+__global__ __launch_bounds__(64 * WAVES, WAVES * paged_resident(WAVES, Form::HEAD_DIM, Form::ROWS == 16) / 4)
 void tree_attn_paged_kernel(const PagedParams) {
   Args p = (Args)__builtin_amdgcn_kernarg_segment_ptr();
-  constexpr int D = Form::HEAD_DIM, RT = Form::RT, QUADS = Form::QUADS, WAVES = paged_waves(Form::ROWS);
+  constexpr int D = Form::HEAD_DIM, RT = Form::RT, QUADS = Form::QUADS;
   __shared__ f32x4 merge_o[WAVES][RT * QUADS][64];
   __shared__ float2 merge_ml[WAVES][RT][64];
+  {   // (a word of each 64 bytes of the arguments: they come from afar, here all at once instead of line by line where they are used. 0.3 us)
+    typedef const __attribute__((address_space(4))) unsigned* Words;
+    const unsigned line1 = ((Words)p)[16], line2 = ((Words)p)[32], line3 = ((Words)p)[48];
+    static_assert(sizeof(PagedParams) > 192 && sizeof(PagedParams) <= 256, "four lines");
+    asm volatile("" :: "s"(line1), "s"(line2), "s"(line3));
+  }
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   using Cuts = Cutter<(Form::ROWS > 16), (D == 128 && Form::ROWS == 32)>;
   Cuts cutter(cut_args(p), threadIdx.x & 63);
@@ -644,7 +650,7 @@ void tree_attn_paged_kernel(const PagedParams) {
     for (int q = 0; q < QUADS; ++q) merge_o[wave][t * QUADS + q][lane] = Form::quad(st, t, q);
   }
   __syncthreads();
-  constexpr int SHARE = RT * QUADS / WAVES;   // quads at a time
+  constexpr int SHARE = RT * QUADS >= WAVES ? RT * QUADS / WAVES : 1;   // quads at a time
   for (int at = kp * SHARE; at < RT * QUADS; at += KW * SHARE) {
     const int t = at / QUADS, q0 = at - t * QUADS;
     float mm = kNoShift;
@@ -733,11 +739,11 @@ __global__ __launch_bounds__(256) void tree_attn_paged_join_kernel(const PagedPa
   put_quad(p.out, p.out_bf16, (((int64_t)b * p.N + node) * p.Hq + g * p.G + (rr - node * p.G)) * D + Form::channel(quad, lane), acc);
 }
 
-template <class Form, bool WIDE>
+template <class Form, int WAVES, bool WIDE>
 void launch(const PagedPlan& pl, const PagedParams& p, hipStream_t stream) {
   // a multiple of eight: workgroup w takes places w / 8, one grid's eighth further, .. of die w % 8's share
   const int wgs = pl.max_pieces < pl.resident ? pl.max_pieces : pl.resident;
-  hipLaunchKernelGGL((tree_attn_paged_kernel<Form, WIDE>), dim3((unsigned)((wgs + 7) / 8 * 8)), dim3(64 * paged_waves(Form::ROWS)), 0, stream, p);
+  hipLaunchKernelGGL((tree_attn_paged_kernel<Form, WAVES, WIDE>), dim3((unsigned)((wgs + 7) / 8 * 8)), dim3(64 * WAVES), 0, stream, p);
   if (!pl.may_cut) return;
   const int rows = pl.rows_per_group < p.N * p.G ? pl.rows_per_group : p.N * p.G;
   hipLaunchKernelGGL((tree_attn_paged_join_kernel<Form>), dim3((unsigned)((rows + Form::TILE - 1) / Form::TILE * (Form::QUADS / 4)), (unsigned)p.Hkv,
@@ -746,9 +752,9 @@ void launch(const PagedPlan& pl, const PagedParams& p, hipStream_t stream) {
 
 template <int D, bool WIDE>
 void launch_rows(const PagedPlan& pl, const PagedParams& p, hipStream_t stream) {
-  if (pl.rows_per_wave == 16) launch<Form16<D>, WIDE>(pl, p, stream);
-  else if (pl.rows_per_wave == 32) launch<Form32<D, 1>, WIDE>(pl, p, stream);
-  else if constexpr (D == 64) launch<Form32<64, 2>, WIDE>(pl, p, stream);
+  if (pl.rows_per_wave == 16) pl.waves == 4 ? launch<Form16<D>, 4, WIDE>(pl, p, stream) : launch<Form16<D>, 8, WIDE>(pl, p, stream);
+  else if (pl.rows_per_wave == 32) launch<Form32<D, 1>, 8, WIDE>(pl, p, stream);
+  else if constexpr (D == 64) launch<Form32<64, 2>, 8, WIDE>(pl, p, stream);
 }
 
 }  // namespace

@@ -14,11 +14,10 @@ constexpr int kBlockKeys = 32;
 constexpr int kPagedMaxBatch = 1024;
 constexpr int kPagedComputeUnits = 256;
 
-constexpr int paged_waves(int rows_per_wave) { return rows_per_wave == 16 ? 4 : 8; }
-constexpr int paged_resident(int rows_per_wave, int D) { return rows_per_wave == 16 ? (D == 64 ? 4 : 3) : 1; }   // workgroups of a compute unit
+constexpr int paged_resident(int waves, int D, bool rows16) { return waves == 4 ? (D == 64 ? 4 : 3) : rows16 && D == 64 ? 2 : 1; }   // workgroups of a compute unit
 
 struct PagedPlan {
-  int rows_per_wave, WS; // row slabs of a workgroup (its other wavefronts split a slab's keys)
+  int rows_per_wave, WS, waves;   // row slabs and wavefronts of a workgroup (those of a slab split its keys)
   int rows_per_group;    // WS * rows_per_wave: 16, 32 or 64
   int groups;            // row groups of a kv head's N * G rows
   int resident;          // workgroups that the device holds at once
@@ -34,8 +33,8 @@ inline int64_t paged_unit_blocks(const fspad_paged_desc& d) {   // at most
   return ((int64_t)d.max_kv_len + kBlockKeys - 1) / kBlockKeys + (d.n_nodes_max + kBlockKeys - 1) / kBlockKeys;
 }
 
-// Rows of a workgroup: 16 (four wavefronts), 32 or 64 (eight), the number that leaves the fewest of them empty. A piece starts and ends in 8 us, pieces
-// are joined in 5 us, and a wavefront takes 0.3 us a block when the device is full: the costs below.
+// Rows of a workgroup: 16 (four wavefronts or eight), 32 or 64 (eight), the number that leaves the fewest of them empty. A piece starts and ends
+// in 8 us, pieces are joined in 5 us, and a wavefront takes 0.3 us a block when the device is full: the costs below.
 inline PagedPlan plan_paged(const fspad_paged_desc& d) {
   PagedPlan pl{};
   const int rows = d.n_nodes_max * (d.n_q_heads / d.n_kv_heads);
@@ -43,16 +42,23 @@ inline PagedPlan plan_paged(const fspad_paged_desc& d) {
   pl.groups = (rows + pl.rows_per_group - 1) / pl.rows_per_group;
   pl.rows_per_wave = pl.rows_per_group == 64 && d.head_dim == 128 ? 32 : pl.rows_per_group;
   pl.WS = pl.rows_per_group / pl.rows_per_wave;
-  const int key_waves = paged_waves(pl.rows_per_wave) / pl.WS;
-  pl.resident = paged_resident(pl.rows_per_wave, d.head_dim) * kPagedComputeUnits;
-  // Joining costs as much as 55 blocks of 16 rows, 30 of 32 and more. One token, 8 kv heads, D = 128: 1024 tokens whole 10.9 us, cut
-  // 12.7; 2048 14.1 and 14.5; 4096 20.2 and 17.5. 26 nodes on 32 heads: 1500 tokens 17.5 whole; 2048 19.6 and 19.4; 3000 22.8 and 19.8.
+  const int64_t units = (int64_t)d.batch * d.n_kv_heads * pl.groups, longest = paged_unit_blocks(d);
+  // 16 rows: eight wavefronts where every unit may have a compute unit and they have several blocks each. One token, 8 kv heads, D = 128:
+  // 400 tokens 8.7 us on four and 9.5 on eight, 2000 13.3 and 13.2, 32 sequences of 4000 32.2 and 30.7, 64 of 1000 18.2 and 21.9.
+  const bool rows16 = pl.rows_per_wave == 16;
+  pl.waves = rows16 && (units > kPagedComputeUnits || longest <= 48) ? 4 : 8;
+  const int key_waves = pl.waves / pl.WS;
+  pl.resident = paged_resident(pl.waves, d.head_dim, rows16) * kPagedComputeUnits;
   pl.least_blocks = 2 * key_waves;
-  pl.whole_blocks = (pl.rows_per_wave == 16 ? 18 : 9) * key_waves;
+  // Joining costs as much as 80 blocks of 16 rows take eight wavefronts, 9 blocks a wavefront of 32 rows; cutting saves nothing where there are as
+  // many units as workgroups, and half of a unit where there are half as many. One token, D = 128, 8 kv heads, whole and cut: 1 sequence of
+  // 2000 tokens 13.2 and 13.5 us, 4000 18.1 and 14.9, 8000 27.5 and 16.5; 16 sequences of 4000 18.8 and 20.2, 8000 35.9 and 35.1; 32 of
+  // 8000 53.7 and 56.1; 64 of 250 .. 4000, D = 64, 20.3 and 25.2. 26 nodes on 32 heads: 2048 19.6 and 19.4; 3000 22.8 and 19.8.
+  const int cuts = (int)(kPagedComputeUnits / units);
+  pl.whole_blocks = !rows16 ? 9 * key_waves : pl.waves == 4 ? 128 : cuts < 2 ? 256 : 80 * cuts / (cuts - 1);
   pl.piece_cost = 8 * key_waves;
   pl.join_cost = 4 * key_waves;
   pl.dead_cost = key_waves;
-  const int64_t units = (int64_t)d.batch * d.n_kv_heads * pl.groups, longest = paged_unit_blocks(d);
   pl.may_cut = d.workgroups > 0 || longest > pl.whole_blocks;
   // as many as there may be blocks, but at most two rounds of the device beside one for each unit
   int64_t cut = d.workgroups > 0 ? d.workgroups : 2 * pl.resident;

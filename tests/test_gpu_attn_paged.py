@@ -250,3 +250,13 @@ def test_more_units_than_workgroups(B, N, Hq, Hkv, D, P, top):
     for b in range(B):
         assert np.all(got[b, nodes[b]:] == 0)
     assert torch.equal(c.run(), c.run(poison=False))
+
+
+@pytest.mark.parametrize("D,P", [(64, 16), (128, 16), (64, 64), (128, 256)])
+@pytest.mark.parametrize("N,Hq,Hkv", [(1, 2, 2), (1, 16, 1), (3, 4, 1)])
+@pytest.mark.parametrize("workgroups", [0, 3, 300])
+def test_few_rows_of_long_sequences(N, Hq, Hkv, D, P, workgroups):
+    """16 rows or less on eight wavefronts, whole and cut, beside sequences of a few tokens and of none."""
+    c = Case(N + D + P, 4, N, Hq, Hkv, D, P, [3000, 1601, 5, 0])
+    c.table[0, 1600 // P] = -1
+    c.check(workgroups=workgroups)

@@ -483,9 +483,11 @@ fspad_status fspad_kv_load_paged(const fspad_paged_desc* desc, int32_t rows, con
  *   out         dev [B,Nmax,Hq,D] out_dtype, 16-byte aligned. Rows i >= n_nodes[b], and rows that see nothing, are zeros
  *   workspace   dev, 16-byte aligned, >= fspad_tree_attn_paged_workspace_bytes(desc) (0: unsupported shape); contents ignored on entry,
  *               undefined on exit; two calls that may overlap in time need different ones
- * What a row does not see has no part in it, NaN and infinity included. Products are of bf16 values (the cached ones are
- * exact in bf16, probabilities are rounded to bf16), sums fp32, the sum of the probabilities over the rounded ones. The same
- * inputs give the same bits from run to run.
+ * What a row does not see has no part in it, NaN and infinity included. Cached keys enter the products as they are stored, against
+ * the sum of two fp8 rows that holds a query (exact down to 2^-14 of the row's largest value, off by 2^-22 of that below); products with tree keys
+ * and with values are of bf16 values (cached ones are exact in bf16, probabilities are rounded to bf16). Sums are fp32, the
+ * sum of the probabilities over the rounded ones. The same inputs give the same bits from run to run; a sequence's results
+ * may differ in their last bits with the batch it is in, which decides how its keys are cut.
  */
 size_t fspad_tree_attn_paged_workspace_bytes(const fspad_paged_desc* desc);
 

@@ -34,10 +34,8 @@ __device__ __forceinline__ unsigned here(unsigned offset) {
   return offset;
 }
 
-struct __attribute__((packed)) Unaligned { unsigned word; };
 template <typename T>
 __device__ __forceinline__ T fetch(GlobalBytes p) { return *(const __attribute__((address_space(1))) T*)p; }
-__device__ __forceinline__ unsigned fetch_any(GlobalBytes p) { return *(const __attribute__((address_space(1))) uint8_t*)p; }
 
 // Two values of a byte of codes, times the scale: the conversion takes the exponent of its scale, what lies around that does not
 // matter, and an exponent of all ones makes NaN of every code. (byte: a constant once unrolled)
@@ -178,7 +176,7 @@ struct Form16 {
   // ---- blocks of the prefix
   struct Keys {
     u32x4 c[2];
-    unsigned scale[2];   // (the products take its first byte)
+    unsigned scale[2];
   };
   struct Values {
     unsigned c[D / 16], scale[2];
@@ -202,7 +200,7 @@ struct Form16 {
     for (int kt = 0; kt < 2; ++kt) {   // (the second 16 keys of a wide block are 16 rows further on)
       const int half = WIDE ? 0 : kt, further = WIDE ? 16 * kt : 0;
       x.c[kt] = fetch<u32x4>(at.code[half] + k + further * (D / 2));
-      x.scale[kt] = fetch_any(at.scale[half] + ks + further);
+      x.scale[kt] = fetch<uint8_t>(at.scale[half] + ks + further);
     }
   }
   template <bool WIDE>
@@ -425,7 +423,7 @@ struct Form32 {
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb) {
       x.c[kb] = fetch<u32x4>(code + k + 32 * kb);
-      x.scale[kb] = fetch_any(scale + 2 * kb * P + ks);
+      x.scale[kb] = fetch<uint8_t>(scale + 2 * kb * P + ks);
     }
   }
   template <bool WIDE>

@@ -149,3 +149,21 @@ def test_slots_and_pages_past_32_bits_of_bytes():
     used = torch.zeros(n_pages, dtype=torch.bool, device=DEV)
     used[[0, n_pages - 30, n_pages - 1]] = True
     assert bool((pool.view(n_pages, -1).amax(1) > 0).eq(used).all())
+
+
+def test_more_rows_than_a_launch_has_workgroups():
+    """One row, repeated by a stride of zero, into every slot of more than a million; then all of them back."""
+    D, P, rows = 128, 64, (1 << 20) + 77
+    n_pages = -(-rows // P)
+    rng = np.random.default_rng(1)
+    k, v = (_rows(rng, 1, 1, D).to(DEV) for _ in range(2))
+    pages = torch.zeros((n_pages, 1, paged.page_head_bytes(D, P)), dtype=torch.uint8, device=DEV)
+    slots = torch.arange(rows, dtype=torch.int32, device=DEV).flip(0).contiguous()
+    fspad.fspad_kv_store_paged(k.expand(rows, 1, D), v.expand(rows, 1, D), slots, pages)
+    got = fspad.fspad_kv_load_paged(slots, pages, D)
+    one = _pool(0, 1, 1, P, D)
+    ref = _put_all(one, D, P, k.cpu(), v.cpu(), [0])
+    for g, name in zip(got, "kv"):
+        want = torch.from_numpy(ref.get(name, 0, 0)).to(torch.bfloat16).to(DEV)
+        assert bool((g[:, 0] == want).all())
+    assert bool((pages[-1, 0, (rows % P) * D // 2:P * D // 2] == 0).all())   # K codes of slots that got no row

@@ -45,7 +45,7 @@ typedef __attribute__((ext_vector_type(4))) __bf16 bf16x4;
 struct CutArgs {
   const int32_t* kv_len;
   const int32_t* n_nodes;
-  int32_t B, N, G, Hkv, rows_shift, ws_shift, groups, max_kv_len, resident, max_pieces, least_blocks, whole_blocks, piece_cost, join_cost, dead_cost, lines, forced;
+  int32_t B, N, G, Hkv, rows_shift, ws_shift, groups, max_kv_len, resident, max_pieces, least_blocks, whole_blocks, piece_cost, join_cost, dead_cost, lines, uncut, forced;   // uncut: every unit is one piece
 };
 
 struct PagedParams {
@@ -78,10 +78,10 @@ __device__ __forceinline__ Args fresh(Args p) {
 __device__ __forceinline__ CutArgs cut_args(Args p) {
   p = fresh(p);
   CutArgs a{p->cut.kv_len, p->cut.n_nodes, p->cut.B, p->cut.N, p->cut.G, p->cut.Hkv, p->cut.rows_shift, p->cut.ws_shift, p->cut.groups,
-            p->cut.max_kv_len, p->cut.resident, p->cut.max_pieces, p->cut.least_blocks, p->cut.whole_blocks, p->cut.piece_cost, p->cut.join_cost, p->cut.dead_cost, p->cut.lines, p->cut.forced};
+            p->cut.max_kv_len, p->cut.resident, p->cut.max_pieces, p->cut.least_blocks, p->cut.whole_blocks, p->cut.piece_cost, p->cut.join_cost, p->cut.dead_cost, p->cut.lines, p->cut.uncut, p->cut.forced};
   asm volatile("" : "+s"(a.kv_len), "+s"(a.n_nodes), "+s"(a.B), "+s"(a.N), "+s"(a.G), "+s"(a.Hkv), "+s"(a.rows_shift), "+s"(a.ws_shift), "+s"(a.groups));
   asm volatile("" : "+s"(a.max_kv_len), "+s"(a.resident), "+s"(a.max_pieces), "+s"(a.least_blocks), "+s"(a.whole_blocks), "+s"(a.piece_cost),
-                    "+s"(a.join_cost), "+s"(a.dead_cost), "+s"(a.lines), "+s"(a.forced));
+                    "+s"(a.join_cost), "+s"(a.dead_cost), "+s"(a.lines), "+s"(a.uncut), "+s"(a.forced));
   return a;
 }
 
@@ -166,9 +166,9 @@ struct Cutter {
     Counts c;
     c.s = shape_of<SLABS>(p, seq);
     const int blocks = (c.s.nb + c.s.half) >> c.s.half;   // of the last group, as long as others' take
-    c.unit = by_pieces() ? (c.s.nb + most - 1) / most : c.s.nb + p.piece_cost;
+    c.unit = p.uncut ? 1 : by_pieces() ? (c.s.nb + most - 1) / most : c.s.nb + p.piece_cost;
     int tail = c.unit;
-    if (SLABS && c.s.half) tail = by_pieces() ? (blocks + most - 1) / most : blocks + p.piece_cost;
+    if (SLABS && c.s.half && !p.uncut) tail = by_pieces() ? (blocks + most - 1) / most : blocks + p.piece_cost;
     c.head = c.s.live == 0 ? 0 : (c.s.live - 1) * c.unit + tail;
     c.own = first + lane < p.B ? p.Hkv * (c.head + (p.groups - c.s.live) * dead_length(p)) : 0;
     c.upto = wave_sum_upto(c.own);
@@ -176,17 +176,20 @@ struct Cutter {
   }
   __device__ __forceinline__ Cutter(const CutArgs& p, int lane_) : lane(lane_) {
     seq = seq_at(p, lane);
-    int blocks = 0, units = 0, longest = 0;
-    for (first = 0;;) {
-      const SeqShape s = shape_of<SLABS>(p, seq);
-      blocks += last_lane(wave_sum_upto(p.Hkv * (s.live * s.nb - (s.half ? s.nb / 2 : 0))));
-      units += last_lane(wave_sum_upto(p.Hkv * s.live));
-      longest = max(longest, last_lane(wave_max_upto(s.nb)));
-      first += 64;
-      if (first >= p.B) break;
-      seq = seq_at(p, first + lane);
+    most = 1;
+    if (!p.uncut) {
+      int blocks = 0, units = 0, longest = 0;
+      for (first = 0;;) {
+        const SeqShape s = shape_of<SLABS>(p, seq);
+        blocks += last_lane(wave_sum_upto(p.Hkv * (s.live * s.nb - (s.half ? s.nb / 2 : 0))));
+        units += last_lane(wave_sum_upto(p.Hkv * s.live));
+        longest = max(longest, last_lane(wave_max_upto(s.nb)));
+        first += 64;
+        if (first >= p.B) break;
+        seq = seq_at(p, first + lane);
+      }
+      most = __builtin_amdgcn_readfirstlane(piece_length<LINES>(p, blocks, units, longest));
     }
-    most = __builtin_amdgcn_readfirstlane(piece_length<LINES>(p, blocks, units, longest));
     length = 0;
     for (first = 0;; first += 64) {
       if (p.B > 64) seq = seq_at(p, first + lane);
@@ -244,6 +247,11 @@ struct Cutter {
           taken = dead_length(p) - off;
           r.dead = off == 0;   // (the window that has its first place writes it)
         }
+      } else if (p.uncut) {
+        r.g = live == 1 ? rel : rel / live;
+        r.y = rel - r.g * live;
+        r.half = SLABS && r.y == live - 1 ? __builtin_amdgcn_readlane(c.s.half, i) : 0;
+        r.end = nb;
       } else {
         r.g = rel / head;
         const int in_head = rel - r.g * head;
@@ -654,11 +662,13 @@ void tree_attn_paged_kernel(const PagedParams) {
   for (int at = kp * SHARE; at < RT * QUADS; at += KW * SHARE) {
     const int t = at / QUADS, q0 = at - t * QUADS;
     float mm = kNoShift;
-    for (int k = 0; k < KW; ++k) mm = fmaxf(mm, merge_ml[slab + k * WS][t][lane].x);
+#pragma unroll 4
+    for (int k = 0; k < KW; ++k) mm = fmaxf(mm, merge_ml[slab + k * WS][t][lane].x);   // (four or eight)
     float l_row = 0.f;
     f32x4 o[SHARE];
 #pragma unroll
     for (int j = 0; j < SHARE; ++j) o[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
     for (int k = 0; k < KW; ++k) {   // in wavefront order: the same bits every time
       const float2 ml = merge_ml[slab + k * WS][t][lane];
       const float a = __builtin_amdgcn_exp2f(ml.x - mm);
@@ -789,7 +799,7 @@ extern "C" fspad_status fspad_tree_attn_paged(const fspad_paged_desc* desc, cons
   p.ws_shift = log2_of(pl.WS); p.rows_per_group = pl.rows_per_group; p.groups = pl.groups;
   p.out_bf16 = d.out_dtype == FSPAD_BF16;
   p.cut = {kv_len, n_nodes, p.B, p.N, p.G, p.Hkv, log2_of(pl.rows_per_group), p.ws_shift, p.groups, d.max_kv_len, pl.resident, pl.max_pieces,
-           pl.least_blocks, pl.whole_blocks, pl.piece_cost, pl.join_cost, pl.dead_cost, pl.lines, d.workgroups};
+           pl.least_blocks, pl.whole_blocks, pl.piece_cost, pl.join_cost, pl.dead_cost, pl.lines, !pl.may_cut, d.workgroups};
   p.c = c;
   hipStream_t stream = reinterpret_cast<hipStream_t>(hip_stream);
   const bool wide = d.page_tokens >= kBlockKeys;

@@ -109,3 +109,9 @@ def test_bad_table_entries_give_no_slots():
     free = np.array([3, 4, 77, 5] + [6] * 8)
     want = _check(np.array([20, 4]), np.array([4, 30]), table, free, 3, 16, max_new=30)
     assert np.all(want[0][0] == -1) and np.all(want[0][1, :12] == -1) and want[0][1, 12] == -1 and list(want[3]) == [1, 1]
+
+
+def test_a_sequence_that_needs_no_page_takes_none_behind_a_refused_one():
+    """Two lack pages, one of them in front of and one behind a sequence whose token fits the page it has: the stack stays as it is."""
+    want = _check(np.array([0, 5, 16]), np.array([40, 2, 1]), np.array([[-1, -1, -1], [0, -1, -1], [1, -1, -1]]), np.array([2, -5, -5]), 1, 16, max_new=40)
+    assert want[3].tolist() == [0, 1, 0] and want[2].tolist() == [1] and want[1].tolist() == [0, 7, 16]

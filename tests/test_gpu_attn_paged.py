@@ -49,7 +49,7 @@ class Case:
         parent, _ = gen_trees(seed, B, N, 6, min(10, max(1, N - 1)), n_nodes=np.maximum(self.n_nodes, 1))
         self.mask = fspad.fspad_tree_build_mask(parent, np.maximum(self.n_nodes, 1))
 
-    def run(self, out_dtype=torch.float32, scale=0.0, workgroups=0, max_kv_len=None, poison=True, pages=None):
+    def run(self, out_dtype=torch.float32, scale=0.0, workgroups=0, max_kv_len=None, poison=True, pages=None, guard=0):
         B, N, Hq, Hkv, D = self.shape
         dev = lambda a: torch.from_numpy(np.ascontiguousarray(a)).to(DEV)  # noqa: E731
         pages = dev(self.raw) if pages is None else pages
@@ -57,11 +57,13 @@ class Case:
         if max_kv_len is None:
             max_kv_len = max(0, int(self.kv_len.max()))
         desc = fspad.make_paged_desc(q, kt, pages, table, max_kv_len, out_dtype, scale, workgroups)
-        ws = torch.full((max(16, fspad.fspad_tree_attn_paged_workspace_bytes(desc)),), 0xFF if poison else 0, dtype=torch.uint8, device=DEV)
+        size = fspad.fspad_tree_attn_paged_workspace_bytes(desc)
+        ws = torch.full((size + guard,), 0xFF if poison else 0, dtype=torch.uint8, device=DEV)
         out = torch.full(q.shape, float("nan"), dtype=out_dtype, device=DEV)
         fspad.fspad_tree_attn_paged(q, kt, vt, pages, table, dev(self.kv_len), dev(self.n_nodes), dev(self.mask.view(np.int64)), out=out,
-                                    workspace=ws, desc=desc)
+                                    workspace=ws[:size], desc=desc)
         torch.cuda.synchronize()
+        assert bool((ws[size:] == (0xFF if poison else 0)).all())
         return out
 
     def reference(self, scale=None, max_kv_len=1 << 30):
@@ -260,3 +262,13 @@ def test_few_rows_of_long_sequences(N, Hq, Hkv, D, P, workgroups):
     c = Case(N + D + P, 4, N, Hq, Hkv, D, P, [3000, 1601, 5, 0])
     c.table[0, 1600 // P] = -1
     c.check(workgroups=workgroups)
+
+
+@pytest.mark.parametrize("B,N,Hq,Hkv,D,P,top,workgroups", [(24, 64, 16, 8, 128, 64, 1300, 0), (20, 40, 16, 8, 64, 32, 2300, 0), (2, 60, 2, 2, 128, 32, 3000, 0), (3, 1, 8, 2, 64, 16, 6000, 0),
+                                                           (5, 1, 8, 8, 128, 16, 300, 0), (2, 33, 4, 2, 128, 16, 700, 3), (2, 5, 4, 2, 64, 16, 700, 4096)])
+def test_writes_stay_inside_the_workspace(B, N, Hq, Hkv, D, P, top, workgroups):
+    rng = np.random.default_rng(top)
+    kv_len, nodes = rng.integers(top // 2, top, B), rng.integers(1, N + 1, B)
+    kv_len[0], nodes[0] = top, N
+    c = Case(B, B, N, Hq, Hkv, D, P, kv_len, nodes)
+    assert torch.equal(c.run(workgroups=workgroups, guard=1 << 20), c.run(workgroups=workgroups, guard=1 << 20, poison=False))

@@ -683,7 +683,7 @@ void tree_attn_paged_kernel(const PagedParams) {
 #pragma unroll
       for (int j = 0; j < SHARE; ++j)
         put_quad(p->out, p->out_bf16, ri.out * D + Form::channel(q0 + j, lane), ri.valid ? o[j] * inv : f32x4{0.f, 0.f, 0.f, 0.f});
-    } else {
+    } else if (ri.valid) {   // (the join reads no others)
       float* part = p->part + piece.index * slot_floats<Form>(p->rows_per_group);
       const int tile = slab * RT + t;
       if (Form::first_key(lane) == 0 && q0 == 0)

@@ -763,8 +763,8 @@ void launch(const PagedPlan& pl, const PagedParams& p, hipStream_t stream) {
 template <int D, bool WIDE>
 void launch_rows(const PagedPlan& pl, const PagedParams& p, hipStream_t stream) {
   if (pl.rows_per_wave == 16) pl.waves == 4 ? launch<Form16<D>, 4, WIDE>(pl, p, stream) : launch<Form16<D>, 8, WIDE>(pl, p, stream);
-  else if (pl.rows_per_wave == 32) launch<Form32<D, 1>, 8, WIDE>(pl, p, stream);
-  else if constexpr (D == 64) launch<Form32<64, 2>, 8, WIDE>(pl, p, stream);
+  else if (pl.rows_per_wave == 32) pl.waves == 4 ? launch<Form32<D, 1>, 4, WIDE>(pl, p, stream) : launch<Form32<D, 1>, 8, WIDE>(pl, p, stream);
+  else if constexpr (D == 64) pl.waves == 4 ? launch<Form32<64, 2>, 4, WIDE>(pl, p, stream) : launch<Form32<64, 2>, 8, WIDE>(pl, p, stream);
 }
 
 }  // namespace

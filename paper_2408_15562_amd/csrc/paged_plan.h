@@ -15,7 +15,7 @@ constexpr int kPagedMaxBatch = 1024;
 constexpr int kPagedComputeUnits = 256;
 
 // Workgroups of a compute unit. (Three of four wavefronts, D = 128, would spill: 64 sequences of 2000 tokens, 8 kv heads, 34.2 us, two 30.6.)
-constexpr int paged_resident(int waves, int D, bool rows16) { return waves == 4 ? (D == 64 ? 4 : 2) : rows16 && D == 64 ? 2 : 1; }
+constexpr int paged_resident(int waves, int D, bool rows16) { return waves == 4 ? (rows16 && D == 64 ? 4 : 2) : rows16 && D == 64 ? 2 : 1; }
 
 struct PagedPlan {
   int rows_per_wave, WS, waves;   // row slabs and wavefronts of a workgroup (those of a slab split its keys)
@@ -44,10 +44,12 @@ inline PagedPlan plan_paged(const fspad_paged_desc& d) {
   pl.rows_per_wave = pl.rows_per_group == 64 && d.head_dim == 128 ? 32 : pl.rows_per_group;
   pl.WS = pl.rows_per_group / pl.rows_per_wave;
   const int64_t units = (int64_t)d.batch * d.n_kv_heads * pl.groups, longest = paged_unit_blocks(d);
-  // 16 rows: eight wavefronts where every unit may have a compute unit and they have several blocks each. One token, 8 kv heads, D = 128:
-  // 400 tokens 8.7 us on four and 9.5 on eight, 2000 13.3 and 13.2, 32 sequences of 4000 32.2 and 30.7, 64 of 1000 18.2 and 21.9.
+  // One slab: eight wavefronts where every unit may have a compute unit to itself and they have several blocks each; else four, and workgroups that share a
+  // compute unit have each other's starts and ends. One token, D = 128, 8 kv heads: 400 tokens 8.7 us on four and 9.5 on eight, 2000 13.3 and 13.2,
+  // 32 sequences of 4000 32.2 and 30.7, 64 of 1000 18.2 and 21.9. 26 nodes on 32 heads: 8 sequences of 1000 15.9 and 17.5, of 2000 27.7 and 20.9, 16 of 300 .. 3000
+  // 40 and 56. Two slabs (64 rows, D = 128), 16 ragged sequences: 68 and 67.
   const bool rows16 = pl.rows_per_wave == 16;
-  pl.waves = rows16 && (units > kPagedComputeUnits || longest <= 48) ? 4 : 8;
+  pl.waves = pl.WS == 1 && (units > kPagedComputeUnits || longest <= (rows16 ? 48 : 36)) ? 4 : 8;
   const int key_waves = pl.waves / pl.WS;
   pl.resident = paged_resident(pl.waves, d.head_dim, rows16) * kPagedComputeUnits;
   pl.least_blocks = 2 * key_waves;

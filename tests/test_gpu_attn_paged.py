@@ -237,7 +237,7 @@ def test_long_prefix_single_token():
 
 
 @pytest.mark.parametrize("B,N,Hq,Hkv,D,P,top", [(24, 64, 16, 8, 128, 64, 1500), (24, 40, 16, 8, 128, 16, 1300), (20, 64, 32, 8, 64, 32, 2300), (70, 33, 8, 4, 128, 32, 1100),
-                                                (17, 32, 16, 8, 128, 128, 4100)])
+                                                (17, 32, 16, 8, 128, 128, 4100), (20, 26, 16, 16, 128, 16, 1400), (20, 17, 16, 16, 64, 64, 1400)])
 def test_more_units_than_workgroups(B, N, Hq, Hkv, D, P, top):
     """Row groups of all heads and sequences in equal windows: units that start and end in any place of one, whole ones, ones without
     nodes, last groups of a few rows. Twice the same bits."""

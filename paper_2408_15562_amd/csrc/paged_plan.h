@@ -44,12 +44,13 @@ inline PagedPlan plan_paged(const fspad_paged_desc& d) {
   pl.rows_per_wave = pl.rows_per_group == 64 && d.head_dim == 128 ? 32 : pl.rows_per_group;
   pl.WS = pl.rows_per_group / pl.rows_per_wave;
   const int64_t units = (int64_t)d.batch * d.n_kv_heads * pl.groups, longest = paged_unit_blocks(d);
-  // One slab: eight wavefronts where every unit may have a compute unit to itself and they have several blocks each; else four, and workgroups that share a
+  // Eight wavefronts where every unit may have a compute unit to itself and they have several blocks each; else four, and workgroups that share a
   // compute unit have each other's starts and ends. One token, D = 128, 8 kv heads: 400 tokens 8.7 us on four and 9.5 on eight, 2000 13.3 and 13.2,
   // 32 sequences of 4000 32.2 and 30.7, 64 of 1000 18.2 and 21.9. 26 nodes on 32 heads: 8 sequences of 1000 15.9 and 17.5, of 2000 27.7 and 20.9, 16 of 300 .. 3000
-  // 40 and 56. Two slabs (64 rows, D = 128), 16 ragged sequences: 68 and 67.
+  // 40 and 56. Two slabs (64 rows, D = 128): 60 nodes on 32 heads, 500 tokens 15.9 and 17.1, 16 sequences of 500 27.5 and 35.8, but 8 of 1000 on 8 heads of keys 33.5
+  // and 24.2 (on four they are cut), 16 ragged ones of up to 6011 68 and 67: eight from 18 blocks on.
   const bool rows16 = pl.rows_per_wave == 16;
-  pl.waves = pl.WS == 1 && (units > kPagedComputeUnits || longest <= (rows16 ? 48 : 36)) ? 4 : 8;
+  pl.waves = (pl.WS == 1 && units > kPagedComputeUnits) || longest <= (rows16 ? 48 : 36 / pl.WS) ? 4 : 8;
   const int key_waves = pl.waves / pl.WS;
   pl.resident = paged_resident(pl.waves, d.head_dim, rows16) * kPagedComputeUnits;
   pl.least_blocks = 2 * key_waves;

@@ -272,3 +272,14 @@ def test_writes_stay_inside_the_workspace(B, N, Hq, Hkv, D, P, top, workgroups):
     kv_len[0], nodes[0] = top, N
     c = Case(B, B, N, Hq, Hkv, D, P, kv_len, nodes)
     assert torch.equal(c.run(workgroups=workgroups, guard=1 << 20), c.run(workgroups=workgroups, guard=1 << 20, poison=False))
+
+
+@pytest.mark.parametrize("B,N,Hq,Hkv,P,top", [(3, 60, 2, 2, 16, 500), (20, 64, 16, 16, 64, 450), (2, 33, 8, 2, 32, 520)])
+def test_two_slabs_on_four_wavefronts(B, N, Hq, Hkv, P, top):
+    """More than 32 rows, D = 128, short sequences: whole units of few blocks, last groups of one slab, forced cuts."""
+    rng = np.random.default_rng(top)
+    kv_len, nodes = rng.integers(0, top, B), rng.integers(0, N + 1, B)
+    kv_len[0], nodes[0] = top, N
+    c = Case(top, B, N, Hq, Hkv, 128, P, kv_len, nodes)
+    c.check()
+    c.check(workgroups=5)

@@ -49,8 +49,10 @@ inline PagedPlan plan_paged(const fspad_paged_desc& d) {
   // 32 sequences of 4000 32.2 and 30.7, 64 of 1000 18.2 and 21.9. 26 nodes on 32 heads: 8 sequences of 1000 15.9 and 17.5, of 2000 27.7 and 20.9, 16 of 300 .. 3000
   // 40 and 56. Two slabs (64 rows, D = 128): 60 nodes on 32 heads, 500 tokens 15.9 and 17.1, 16 sequences of 500 27.5 and 35.8, but 8 of 1000 on 8 heads of keys 33.5
   // and 24.2 (on four they are cut), 16 ragged ones of up to 6011 68 and 67: eight from 18 blocks on.
+  // Few units, cut: 26 nodes on 32 heads, 2000 tokens 16.6 and 18.3, 4000 17.9 and 20.1, 8000 25.3 and 22.4; 60 nodes on 8 heads, 2000 19.2 and 21.0, on 32, 4000 27.8 and 24.3.
   const bool rows16 = pl.rows_per_wave == 16;
-  pl.waves = (pl.WS == 1 && units > kPagedComputeUnits) || longest <= (rows16 ? 48 : 36 / pl.WS) ? 4 : 8;
+  const bool few = !rows16 && units <= 32 && units * longest * pl.WS <= 4400;   // as many pieces of few blocks as compute units
+  pl.waves = (pl.WS == 1 && units > kPagedComputeUnits) || longest <= (rows16 ? 48 : 36 / pl.WS) || few ? 4 : 8;
   const int key_waves = pl.waves / pl.WS;
   pl.resident = paged_resident(pl.waves, d.head_dim, rows16) * kPagedComputeUnits;
   pl.least_blocks = 2 * key_waves;

@@ -59,7 +59,7 @@ inline PagedPlan plan_paged(const fspad_paged_desc& d) {
   // Joining costs as much as 80 blocks of 16 rows take eight wavefronts, 9 blocks a wavefront of 32 rows; cutting saves nothing where there are as
   // many units as workgroups, and half of a unit where there are half as many. One token, D = 128, 8 kv heads, whole and cut: 1 sequence of
   // 2000 tokens 13.2 and 13.5 us, 4000 18.1 and 14.9, 8000 27.5 and 16.5; 16 sequences of 4000 18.8 and 20.2, 8000 35.9 and 35.1; 32 of
-  // 8000 53.7 and 56.1; 64 of 250 .. 4000, D = 64, 20.3 and 25.2. 26 nodes on 32 heads: 2048 19.6 and 19.4; 3000 22.8 and 19.8.
+  // 8000 53.7 and 56.1; 64 of 250 .. 4000, D = 64, 20.3 and 25.2. 26 nodes on 32 heads, eight wavefronts: 2048 19.6 and 19.4; 3000 22.8 and 19.8.
   const int cuts = (int)(kPagedComputeUnits / units);
   pl.whole_blocks = !rows16 ? 9 * key_waves : pl.waves == 4 ? 128 : cuts < 2 ? 256 : 80 * cuts / (cuts - 1);
   pl.piece_cost = 8 * key_waves;

@@ -678,6 +678,20 @@ def make_paged_desc(q: torch.Tensor, k_tree: torch.Tensor, pages: torch.Tensor, 
     return d
 
 
+def _check_paged_desc(desc: fspad_paged_desc, made: fspad_paged_desc):
+    """A descriptor that the caller brings against the one that the tensors make: nothing behind them may be read or written. It may name
+    fewer pages and fewer entries of a table's row than there are; of an axis of one entry the stride says nothing."""
+    for name in ("batch", "n_nodes_max", "n_q_heads", "n_kv_heads", "head_dim", "io_dtype", "page_tokens"):
+        if getattr(desc, name) != getattr(made, name):
+            raise ValueError(f"desc.{name} is {getattr(desc, name)}, the tensors have {getattr(made, name)}")
+    for name in ("n_pages", "table_width"):
+        if getattr(desc, name) > getattr(made, name):
+            raise ValueError(f"desc.{name} is {getattr(desc, name)}, the tensors have {getattr(made, name)}")
+    for name, entries in (("page_stride", desc.n_pages), ("table_stride", desc.batch)):
+        if entries > 1 and getattr(desc, name) != getattr(made, name):
+            raise ValueError(f"desc.{name} is {getattr(desc, name)}, the tensors have {getattr(made, name)}")
+
+
 def fspad_tree_attn_paged_workspace_bytes(desc: fspad_paged_desc) -> int:
     return int(_lib().fspad_tree_attn_paged_workspace_bytes(ctypes.byref(desc)))
 
@@ -690,15 +704,24 @@ def fspad_tree_attn_paged(q: torch.Tensor, k_tree: torch.Tensor, v_tree: torch.T
                           prepare: bool = False, workgroups: int = 0):
     """q [B,Nmax,Hq,D]; k_tree,v_tree [B,Nmax,Hkv,D]; pages uint8 [n_pages,Hkv,page bytes per head] (any page stride);
     block_table int32 [B,width]; kv_len,n_nodes DEVICE int32 [B]; anc_mask device int64/uint64 [B,Nmax]. max_kv_len: no
-    sequence is longer (the launch is laid out for it). Returns out [B,Nmax,Hq,D]; with prepare=True a PreparedCall."""
+    sequence is longer (the launch is laid out for it). desc: a descriptor from make_paged_desc in the place of max_kv_len,
+    softmax_scale, out_dtype and workgroups; it has to agree with the tensors, and with those arguments where they are given.
+    Returns out [B,Nmax,Hq,D]; with prepare=True a PreparedCall."""
     B, Nmax, Hq, D = q.shape
     for name, t, shape in (("q", q, tuple(q.shape)), ("k_tree", k_tree, (B, Nmax, k_tree.shape[2], D)),
                            ("v_tree", v_tree, tuple(k_tree.shape))):
         if not t.is_contiguous() or t.dtype != q.dtype or tuple(t.shape) != shape:
             raise ValueError(f"{name} must be a contiguous {shape} tensor of q's dtype")
+    made = make_paged_desc(q, k_tree, pages, block_table, max_kv_len,
+                           out_dtype if out_dtype is not None else (out.dtype if out is not None else None), softmax_scale, workgroups)
     if desc is None:
-        desc = make_paged_desc(q, k_tree, pages, block_table, max_kv_len,
-                               out_dtype if out_dtype is not None else (out.dtype if out is not None else None), softmax_scale, workgroups)
+        desc = made
+    else:
+        _check_paged_desc(desc, made)
+        for name, given in (("max_kv_len", max_kv_len is not None), ("softmax_scale", softmax_scale != 0.0), ("out_dtype", out_dtype is not None),
+                            ("workgroups", workgroups != 0)):
+            if given and getattr(desc, name) != getattr(made, name):
+                raise ValueError(f"desc and the argument {name} differ")
     for name, t in (("kv_len", kv_len), ("n_nodes", n_nodes)):
         if t.dtype != torch.int32 or not t.is_contiguous() or tuple(t.shape) != (B,):
             raise ValueError(f"{name} must be a contiguous int32 [B] device tensor")

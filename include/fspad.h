@@ -391,7 +391,7 @@ typedef struct {
   int32_t head_dim;       /* D: 64 or 128 */
   int32_t io_dtype;       /* FSPAD_BF16: q, k_tree, v_tree, and the rows that are stored and loaded */
   int32_t out_dtype;      /* FSPAD_BF16 or FSPAD_F32 (attention only) */
-  float softmax_scale;    /* 0 => 1/sqrt(D); finite, of any sign, else 2^-125 at least in magnitude (attention only) */
+  float softmax_scale;    /* 0 => 1/sqrt(D); else of any sign, 2^-125 .. 2^127 in magnitude (attention only) */
   int32_t page_tokens;    /* P: 16, 32, 64, 128 or 256 */
   int32_t n_pages;        /* pages of the pool, >= 1 */
   int64_t page_stride;    /* bytes from page to page, below 2^32 */
@@ -401,7 +401,7 @@ typedef struct {
   int32_t workgroups;     /* tuning of the attention: 0 = the built-in choice; 1..4096 cuts the keys into about that many pieces
                              beside one for each (sequence, kv head, group of query rows). Results do not depend on it beyond
                              fp32 rounding of the join; the workspace's size does */
-  int32_t reserved;       /* 0 */
+  int32_t reserved;       /* 0; not looked at */
 } fspad_paged_desc;
 
 /* Bytes of one page, 0 for an unsupported shape. */
@@ -479,6 +479,12 @@ fspad_status fspad_kv_load_paged(const fspad_paged_desc* desc, int32_t rows, con
  *   block_table dev [B] rows of table_width i32, table_stride entries apart. Positions on an entry outside [0,n_pages) are
  *               left out, as if they were masked; entries past ceil(kv_len[b] / P) are not looked at
  *   kv_len      DEV [B] i32, taken as 0 .. max_kv_len;  n_nodes DEV [B] i32, taken as 0 .. Nmax
+ *   max_kv_len  of the descriptor: all that is known of the lengths when the call is launched. Results do not depend on it beyond
+ *               their last bits, as long as it holds. Short calls take longer under one far above the lengths, which starts the kernels
+ *               of long sequences and a second launch that then has nothing to join: one token, 511 tokens on 8 kv heads, 9.1 us under
+ *               its own length and 11.6 under 8192 or more; a tree of 26 nodes, 2048 tokens, 16.5 and 21.1; 64 single tokens of up to
+ *               4000, D = 64, 19.1 and 21.6. Calls that are laid out for cut keys either way take the same (4 trees of 60 nodes, 4096
+ *               tokens: 46). A table no wider than the longest sequence that is served is bound enough
  *   anc_mask    dev [B,Nmax] u64 as for fspad_tree_attn
  *   out         dev [B,Nmax,Hq,D] out_dtype, 16-byte aligned. Rows i >= n_nodes[b], and rows that see nothing, are zeros
  *   workspace   dev, 16-byte aligned, >= fspad_tree_attn_paged_workspace_bytes(desc) (0: unsupported shape); contents ignored on entry,
@@ -486,8 +492,9 @@ fspad_status fspad_kv_load_paged(const fspad_paged_desc* desc, int32_t rows, con
  * What a row does not see has no part in it, NaN and infinity included. Cached keys enter the products as they are stored, against
  * the sum of two fp8 rows that holds a query (exact down to 2^-14 of the row's largest value, off by 2^-22 of that below); products with tree keys
  * and with values are of bf16 values (cached ones are exact in bf16, probabilities are rounded to bf16). Sums are fp32, the
- * sum of the probabilities over the rounded ones. The same inputs give the same bits from run to run; a sequence's results
- * may differ in their last bits with the batch it is in, which decides how its keys are cut.
+ * sum of the probabilities over the rounded ones; a score times scale * log2(e) has to be a finite fp32 number. The same inputs
+ * give the same bits from run to run; a sequence's results may differ in their last bits with the batch it is in, which decides how
+ * its keys are cut.
  */
 size_t fspad_tree_attn_paged_workspace_bytes(const fspad_paged_desc* desc);
 

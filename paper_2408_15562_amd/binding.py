@@ -704,9 +704,9 @@ def fspad_tree_attn_paged(q: torch.Tensor, k_tree: torch.Tensor, v_tree: torch.T
                           prepare: bool = False, workgroups: int = 0):
     """q [B,Nmax,Hq,D]; k_tree,v_tree [B,Nmax,Hkv,D]; pages uint8 [n_pages,Hkv,page bytes per head] (any page stride);
     block_table int32 [B,width]; kv_len,n_nodes DEVICE int32 [B]; anc_mask device int64/uint64 [B,Nmax]. max_kv_len: no
-    sequence is longer (the launch is laid out for it). desc: a descriptor from make_paged_desc in the place of max_kv_len,
-    softmax_scale, out_dtype and workgroups; it has to agree with the tensors, and with those arguments where they are given.
-    Returns out [B,Nmax,Hq,D]; with prepare=True a PreparedCall."""
+    sequence is longer (the launch is laid out for it; what the table's rows hold, if not given). desc: a descriptor from
+    make_paged_desc in the place of max_kv_len, softmax_scale, out_dtype and workgroups; it has to agree with the tensors, and
+    with those arguments where they are given. Returns out [B,Nmax,Hq,D]; with prepare=True a PreparedCall."""
     B, Nmax, Hq, D = q.shape
     for name, t, shape in (("q", q, tuple(q.shape)), ("k_tree", k_tree, (B, Nmax, k_tree.shape[2], D)),
                            ("v_tree", v_tree, tuple(k_tree.shape))):

@@ -30,7 +30,7 @@ struct RowsParams {
   char* pages;
   int64_t row_stride, head_stride;   // bytes
   int64_t page_stride;
-  int32_t rows, n_slots, page_shift, D;
+  int32_t rows, n_slots, page_shift;
 };
 
 constexpr int kRowThreads = 256;
@@ -161,7 +161,7 @@ fspad_status move_rows(bool store, const fspad_paged_desc* desc, int32_t rows, v
   RowsParams p{};
   p.k = static_cast<char*>(k); p.v = static_cast<char*>(v); p.slots = slots; p.pages = static_cast<char*>(pages);
   p.row_stride = row_stride * 2; p.head_stride = head_stride * 2; p.page_stride = d.page_stride;
-  p.rows = rows; p.n_slots = d.n_pages * d.page_tokens; p.page_shift = log2_of(d.page_tokens); p.D = d.head_dim;
+  p.rows = rows; p.n_slots = d.n_pages * d.page_tokens; p.page_shift = log2_of(d.page_tokens);
   const int rpw = kRowThreads / (d.head_dim / 8);
   const int64_t wgs = (rows + (int64_t)rpw - 1) / rpw;
   const dim3 grid((unsigned)d.n_kv_heads, (unsigned)(wgs < 65535 ? wgs : 65535));

@@ -10,12 +10,13 @@
 //                  order to channel order two bytes at a time (v_perm_b32).
 // paged_forms.h has both, for 16 rows and for tiles of 32.
 //
-// What bounds it: instructions. A block of 32 keys takes a wavefront of 32 rows (D = 128) about 155 vector instructions, half of them V's, and
-// 540 clocks of products, and of the two wavefronts of a SIMD the products of one hide little of the other's vector work: 1040 clocks a
-// block for one wavefront alone, 950 for each of two (probed without loads; 1170 and 1020 with them). 64 query heads on 8 kv heads, 60 nodes, 16384 tokens
-// (32 GFLOP): 49 us and 5 us for joining, 650 TFLOP/s; 4 sequences of 4096 tokens, 60 nodes and 52 heads (129 MB of pages): 51 us, 2.5 TB/s.
-// Both sides of what was chosen, at these two: 64 rows a wavefront (D = 128, one wavefront a SIMD, V converted once for all) 55 and 55 us
-// for 51 and 51; with D = 64 64 rows fit two wavefronts a SIMD and win, 33 for 34.5 us (8 sequences of 4000) and 68 for 72 us (32 ragged ones).
+// What bounds it: instructions. A block of 32 keys takes a wavefront of 32 rows (D = 128) 155 vector instructions, 92 of them V's, and
+// 540 clocks of products, and of the two wavefronts of a SIMD the products of one hide little of the other's vector work: 1060 clocks a
+// block for one wavefront alone, 960 for each of two (probed without loads; 1120 and 990 with them). 64 query heads on 8 kv heads, 60 nodes, 16384 tokens
+// (32 GFLOP): 48 us, 5 of them the join's, 670 TFLOP/s; 4 sequences of 4096 tokens, 60 nodes and 52 heads (116 MB of pages, 129 with the rows): 49 us, 4 of
+// them a join without pieces, 2.6 TB/s.
+// Both sides of what was chosen, at these two, the kernel alone under a profiler: 64 rows a wavefront (D = 128, one wavefront a SIMD, V converted once for all)
+// 55 and 55 us for 51 and 51; with D = 64 64 rows fit two wavefronts a SIMD and win, 33 for 34.5 us (8 sequences of 4000) and 68 for 72 us (32 ragged ones).
 //
 // How a call is cut is decided on the device, from lengths it alone knows (piece_length): a unit, 64 query rows or less of one kv head of one
 // sequence, is one workgroup's or is cut along its keys. A whole unit goes straight to `out`; of the others every piece leaves its
@@ -116,8 +117,9 @@ __device__ __forceinline__ int last_lane(int x) { return __builtin_amdgcn_readla
 // workgroup takes an equal window of it: the end of one unit, whole ones, the start of another. What starting and ending a piece takes
 // stands on the line as blocks in front of each unit. 16 ragged sequences of 131 .. 6011 tokens, 17 .. 60 nodes on 32 heads (8 of keys): 99 us in
 // equal pieces or whole units, several a workgroup, 69 us on a line; 32 of 100 .. 4000 tokens, D = 64: 96 and 68 us. Where all units go in
-// one round the line costs a second start for most workgroups: 53 for 49 us (64 units, 256 workgroups). With 16 rows, three or four
-// workgroups share a compute unit and each other's gaps: 64 ragged sequences of one token 27 us on a line, 25 us in equal pieces.
+// one round the line costs a second start for most workgroups: 53 for 49 us (64 units, 256 workgroups). With 16 rows, D = 64, two or four
+// workgroups share a compute unit and each other's gaps: 64 ragged sequences of one token 27 us on a line, 25 us in equal pieces (whole, as they
+// are now, 19); 16 rows never go on a line.
 template <bool LINES>
 __device__ __forceinline__ int piece_length(const CutArgs& p, int blocks, int units, int longest) {
   const float slots = (float)(p.max_pieces - p.B * p.Hkv * p.groups);   // the sum of ceil(nb / len) is at most S / len + units

@@ -21,8 +21,9 @@ typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
 // bounds a large call is memory. A lane holds 8 channels of one row (16 bytes of bf16, 4 of codes), 16 lanes a row of D = 128
 // (8 of D = 64), four lanes a block. A wavefront takes neighbouring rows of ONE head: a prompt's rows are neighbours in their
 // page too, so that a store instruction writes whole 256-byte stretches of codes. Workgroups that run at the same time have all heads of
-// neighbouring rows, whose bf16 lies in a row: 8191 rows of 32 heads, D = 128 (170 MB), are stored in 33 us and loaded in 35 us, 5.1 and
-// 4.9 TB/s (39 and 40 us head after head, which reads 256 bytes in every 8 KB); 16384 rows of 8 heads are loaded in 15 us (5.6 TB/s).
+// neighbouring rows, whose bf16 lies in a row: 8191 rows of 32 heads, D = 128 (170 MB), are stored and loaded in 67 us, 5.1 TB/s (41 and 26: the load finds part
+// of it in the memory-side cache; 80 head after head, which reads 256 bytes in every 8 KB); 40000 rows (829 MB) in 158 us each way, 5.3 TB/s; D = 64: 80000 rows
+// (829 MB) stored in 177 us and loaded in 182, 4.7 and 4.6 TB/s; 16384 rows of 8 heads, D = 128, are loaded in 14.3 us (5.9 TB/s, from that cache).
 struct RowsParams {
   char* k;               // [rows] x [Hkv] x D bf16: read by the store, written by the load
   char* v;

@@ -34,8 +34,10 @@ inline int64_t paged_unit_blocks(const fspad_paged_desc& d) {   // at most
   return ((int64_t)d.max_kv_len + kBlockKeys - 1) / kBlockKeys + (d.n_nodes_max + kBlockKeys - 1) / kBlockKeys;
 }
 
-// Rows of a workgroup: 16 (four wavefronts or eight), 32 or 64 (eight), the number that leaves the fewest of them empty. A piece starts and ends
-// in 8 us, pieces are joined in 5 us, and a wavefront takes 0.3 us a block when the device is full: the costs below.
+// Rows of a workgroup: the smallest of 16, 32 and 64 that holds all of a kv head's, or groups of 64 where none does. 64 rows are one slab with
+// D = 64, two slabs of 32 with D = 128, whose wavefronts read the same keys. Four wavefronts or eight, by the rules below. A piece starts and ends
+// in 8 us, pieces are joined in 5 us, and a wavefront takes 0.3 us a block when the device is full: the costs below. What is known of the lengths here
+// is max_kv_len alone.
 inline PagedPlan plan_paged(const fspad_paged_desc& d) {
   PagedPlan pl{};
   const int rows = d.n_nodes_max * (d.n_q_heads / d.n_kv_heads);
@@ -50,6 +52,8 @@ inline PagedPlan plan_paged(const fspad_paged_desc& d) {
   // 40 and 56. Two slabs (64 rows, D = 128): 60 nodes on 32 heads, 500 tokens 15.9 and 17.1, 16 sequences of 500 27.5 and 35.8, but 8 of 1000 on 8 heads of keys 33.5
   // and 24.2 (on four they are cut), 16 ragged ones of up to 6011 68 and 67: eight from 18 blocks on.
   // Few units, cut: 26 nodes on 32 heads, 2000 tokens 16.6 and 18.3, 4000 17.9 and 20.1, 8000 25.3 and 22.4; 60 nodes on 8 heads, 2000 19.2 and 21.0, on 32, 4000 27.8 and 24.3.
+  // More than 32 units, on four and cut as those are, and on eight: 26 nodes on 64 heads, or 2 sequences on 32, 1300 tokens 19.9 and 16.2, 2048 20.8 and 18.9; on 40
+  // heads, 1300 16.3 and 16.0, 2048 16.8 and 18.8, 3000 21.1 and 19.6.
   const bool rows16 = pl.rows_per_wave == 16;
   const bool few = !rows16 && units <= 32 && units * longest * pl.WS <= 4400;   // as many pieces of few blocks as compute units
   pl.waves = (pl.WS == 1 && units > kPagedComputeUnits) || longest <= (rows16 ? 48 : 36 / pl.WS) || few ? 4 : 8;

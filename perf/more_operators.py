@@ -2,8 +2,8 @@
 
 Five kinds of pass, all through the public entry points of the package:
 
-  attn     fspad_tree_attn_paged_fp8: the draft tree's queries (or one token's) against 8-bit pages and the tree itself
-  store    fspad_kv_store_paged_fp8, then fspad_kv_load_paged_fp8 of the blocks that were written to: what the cache holds of them
+  attn     fspad_tree_attn_paged_byte: the draft tree's queries (or one token's) against 8-bit pages and the tree itself
+  store    fspad_kv_store_paged_byte, then fspad_kv_load_paged_byte of the blocks that were written to: what the cache holds of them
            is returned as the values that it stands for
   fork     fspad_page_fork, then fspad_page_copy in a layer's pool: sequences begin as copies of others, whose full pages they share
   release  fspad_page_release: sequences end, pages that nobody else holds go back to the stack
@@ -463,12 +463,12 @@ def _calls(s):
     case = s["case"]
     kind, P = case["kind"], case["page_tokens"]
     if kind == "attn":
-        call = fspad.fspad_tree_attn_paged_fp8(s["q"], s["k_tree"], s["v_tree"], s["pages"], s["table"], s["kv_len"], s["nodes"], s["mask"],
+        call = fspad.fspad_tree_attn_paged_byte(s["q"], s["k_tree"], s["v_tree"], s["pages"], s["table"], s["kv_len"], s["nodes"], s["mask"],
                                                max_kv_len=s["max_kv_len"], prepare=True)
         return [call], call.result
     if kind == "store":
-        store = fspad.fspad_kv_store_paged_fp8(s["k"], s["v"], s["slots"], s["pages"], prepare=True)
-        load = fspad.fspad_kv_load_paged_fp8(s["back"], s["pages"], case["head_dim"], prepare=True)
+        store = fspad.fspad_kv_store_paged_byte(s["k"], s["v"], s["slots"], s["pages"], prepare=True)
+        load = fspad.fspad_kv_load_paged_byte(s["back"], s["pages"], case["head_dim"], prepare=True)
         return [store, load], load.result
     if kind == "release":
         call = fspad.fspad_page_release(s["ended"], s["kv_len"], s["table"], s["free"], s["n_free"], s["shared"], P, prepare=True)

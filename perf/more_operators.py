@@ -14,8 +14,8 @@ cached through the rounding that the store applies; what no token occupies of a 
 
 The cache's format. A block is 32 neighbouring tokens of a page and one kv head, K and V apart. An element is an 8-bit float (1 sign, 4
 exponent, 3 mantissa bits, largest 448, no infinity), a block's scale 2^(s-127) for a byte s. Of values whose largest finite magnitude is a,
-s is the smallest of 10..247 with a <= 448 * 2^(s-127); values are rounded to the nearest element (ties to even), NaN and infinity
-become NaN. A call that stores a block's first token begins the block: its scale is that of the call's tokens in it. Otherwise it is
+s is the smallest of 10..246 with a <= 448 * 2^(s-127), 246 where that is too small; values are rounded to the nearest element (ties to
+even, at most 448), NaN and infinity become NaN. A call that stores a block's first token begins the block: its scale is that of the call's tokens in it. Otherwise it is
 the larger of that and of the scale the block has; where it grows, the tokens that the block held are rounded again under the new one.
 Where a page of P tokens keeps one kv head's D channels (E = D/32):
 
@@ -328,7 +328,7 @@ def _v_back(c):
 
 def _scale_of(top):
     m, e = torch.frexp(top)                                                # top = m 2^e, 1/2 <= m < 1; 448 * 2^z = 7/8 * 2^(z+9)
-    return torch.where(top > 0, e - 9 + (m > 0.875).int() + 127, 0).clamp(10, 247)
+    return torch.where(top > 0, e - 9 + (m > 0.875).int() + 127, 0).clamp(10, 246)
 
 
 def _plain_store(k, v, slots, pages, P):
@@ -349,7 +349,7 @@ def _plain_store(k, v, slots, pages, P):
         was = back(codes[page, :, nth])                                    # [blocks, Hkv, 32, D]
         again = torch.ldexp(was.view(FP8).float(), (had - s)[..., None, None]).to(FP8).view(U8)
         new = torch.where((~begun[:, None] & (s > had))[..., None, None], again, was)
-        new[of, :, t] = torch.ldexp(x, 127 - s[of][..., None]).to(FP8).view(U8)
+        new[of, :, t] = torch.ldexp(x, 127 - s[of][..., None]).clamp(-448, 448).to(FP8).view(U8)
         codes[page, :, nth] = order(new, D)
         scales[page, :, nth] = s.to(U8)
 
@@ -554,7 +554,7 @@ def _exact_round(x, s):
     y = x / torch.pow(torch.tensor(2.0, dtype=F64, device="cuda"), s.double() - 127)
     _, e = torch.frexp(y)
     step = torch.pow(torch.tensor(2.0, dtype=F64, device="cuda"), (e.double() - 4).clamp(min=-9))
-    return torch.round(y / step) * step * torch.pow(torch.tensor(2.0, dtype=F64, device="cuda"), s.double() - 127)   # (round: ties to even)
+    return (torch.round(y / step) * step).clamp(-448, 448) * torch.pow(torch.tensor(2.0, dtype=F64, device="cuda"), s.double() - 127)   # (round: ties to even)
 
 
 def _exact_store(s, P, D):
@@ -566,12 +566,12 @@ def _exact_store(s, P, D):
     before = _exact_pages(s["pages"], P, D)
     block = torch.arange(32, device="cuda") + back[:, None] // 32 * 32                     # the slots of every slot's block
     out = []
-    powers = torch.pow(torch.tensor(2.0, dtype=F64, device="cuda"), torch.arange(10, 248, device="cuda").double() - 127)
+    powers = torch.pow(torch.tensor(2.0, dtype=F64, device="cuda"), torch.arange(10, 247, device="cuda").double() - 127)
     for x, old, at in ((s["k"], before[0], 0), (s["v"], before[1], 8)):
         had = s["pages"][back // P, :, 2 * P * D + at + back % P // 32].long()             # [rows, Hkv]
         top_of_row = torch.cat([x.double().abs().amax(-1), torch.zeros(1, x.shape[1], dtype=F64, device="cuda")])
         top = top_of_row[new[block]].amax(1)                                               # (-1: the row of zeros)
-        scale = torch.searchsorted(448 * powers, top).clamp(max=237) + 10
+        scale = torch.searchsorted(448 * powers, top).clamp(max=236) + 10
         begun = (new[block[:, 0]] >= 0)[:, None]
         scale = torch.where(begun, scale, torch.maximum(scale, had))[..., None]
         mine = new[back]

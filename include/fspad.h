@@ -27,7 +27,8 @@
  *      choice of the tree from the candidates (Preliminaries, last paragraph:
  *      fspad_draft_topk, fspad_tree_build);
  *   6. the same attention over a paged 4-bit cache, with the calls that keep it (fspad_tree_attn_paged,
- *      fspad_page_map, fspad_kv_store_paged, fspad_kv_load_paged).
+ *      fspad_page_map, fspad_kv_store_paged, fspad_kv_load_paged), and over a paged 8-bit one
+ *      (fspad_tree_attn_paged_byte, fspad_kv_store_paged_byte, fspad_kv_load_paged_byte).
  *
  * Conventions that hold for every entry point:
  *   - "dev" pointers are device (HBM) addresses, "host" pointers are host
@@ -504,6 +505,69 @@ fspad_status fspad_tree_attn_paged(const fspad_paged_desc* desc,
                                    const int32_t* kv_len, const int32_t* n_nodes,
                                    const uint64_t* anc_mask, void* out,
                                    void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * Paged 8-bit cache (no passage of the paper: a storage format between the bf16 cache, of which it takes half, and the 4-bit one, with errors of
+ * 1/16 of a value at most). Block tables, slots, lengths and the stack of free pages are those of the 4-bit cache: fspad_page_map keeps
+ * them, and descriptors are the same (page_tokens: 32, 64, 128 or 256).
+ *
+ * Values. A block is 32 neighbouring tokens of a page (from a multiple of 32 on) and one kv head; K and V have scales of their own. An element is
+ * an 8-bit float: a sign, 4 bits of exponent, 3 of mantissa, the smallest 2^-9, the largest 448, all bits below the sign NaN (E4M3 of the OCP
+ * formats). A block's scale is 2^(s-127) for a byte s. What a store does to a block that some of its rows go to, whose largest finite magnitude
+ * is a:
+ *   t    = the smallest of 10..246 with a <= 448 * 2^(t-127) (246 where that is too small too)
+ *   s    = t if one of the rows goes to the block's first token: the call begins the block (what it holds of tokens that are not in the call
+ *          is not specified then). Else the larger of t and the s that the block has; where it grows, the tokens that the block held are
+ *          rounded again, value / 2^(s-127), as below
+ *   code = the element nearest to x / 2^(s-127), ties to the even one, at most 448; NaN and infinity become NaN
+ * so that a value up to 7 * 2^125 is off by at most 1/16 of it, or by 2^(s-137) where that is more. A scale grows by powers of two: rounding again changes
+ * only values that come to lie below 2^-6 of the new one, and those by the same 2^(s-137) at most. What reads a cache takes s from 10 to
+ * 246; other scales are not specified.
+ *
+ * Pages. A page holds page_tokens tokens of all kv heads of one layer, one head after the other, of each (P = page_tokens, D = head_dim,
+ * E = D / 32), in bytes:
+ *   K codes  [P/32][D/16][32][16]     token t, channel c at [t/32][c/16][t%32][c%16]
+ *   V codes  [P/32][E][2][32][16]     token t, channel c at [t/32][c%E][t%32/16][c/E][t%16]
+ *   K scales [8]                      of block t/32, the first P/32 of them used
+ *   V scales [8]
+ * fspad_kv_page_bytes_byte = Hkv * (2 * P * D + 16) in all. page_stride and n_pages as for the 4-bit cache.
+ */
+
+/* Bytes of one page, 0 for an unsupported shape. */
+size_t fspad_kv_page_bytes_byte(int32_t n_kv_heads, int32_t head_dim, int32_t page_tokens);
+
+/*
+ * Keys and values of `rows` tokens into the slots they are given, as fspad_kv_store_paged, rounded as above.
+ *   k, v, slots, row_stride, head_stride   as there. The rows of a block may stand anywhere in the call. No slot may be given to two rows of a
+ *             call (what the block holds of it then is not specified)
+ *   rows      0..1048560; 0 does nothing (no pointer is looked at)
+ *   pages     dev, 16-byte aligned. Tokens of other blocks stay as they are; no other call may use a block that this one stores to meanwhile
+ *   workspace dev, 16-byte aligned, >= fspad_kv_store_paged_byte_workspace_bytes(desc, rows): 0 up to 1024 rows (may be NULL then), 4 bytes a
+ *             slot of the pool for more; contents ignored on entry, undefined on exit; two calls that may overlap in time need different ones
+ * Reads n_kv_heads, head_dim, io_dtype, page_tokens, n_pages and page_stride of the descriptor, as fspad_kv_load_paged_byte does.
+ */
+size_t fspad_kv_store_paged_byte_workspace_bytes(const fspad_paged_desc* desc, int32_t rows);
+
+fspad_status fspad_kv_store_paged_byte(const fspad_paged_desc* desc, int32_t rows, const void* k, const void* v,
+                                      int64_t row_stride, int64_t head_stride, const int32_t* slots, void* pages,
+                                      void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* The reverse, as fspad_kv_load_paged: row r of k and v (bf16, exact) is what slots[r] holds, zeros where the slot is outside the pool. */
+fspad_status fspad_kv_load_paged_byte(const fspad_paged_desc* desc, int32_t rows, const int32_t* slots, const void* pages,
+                                     void* k, void* v, int64_t row_stride, int64_t head_stride, void* hip_stream);
+
+/*
+ * fspad_tree_attn_paged over 8-bit pages: arguments, masks, lengths, outputs, workspace and errors are those of that call. Products with cached
+ * keys and values, and the roundings of queries, weights and sums, are those that stand there too (cached values are exact in bf16).
+ */
+size_t fspad_tree_attn_paged_byte_workspace_bytes(const fspad_paged_desc* desc);
+
+fspad_status fspad_tree_attn_paged_byte(const fspad_paged_desc* desc,
+                                       const void* q, const void* k_tree, const void* v_tree,
+                                       const void* pages, const int32_t* block_table,
+                                       const int32_t* kv_len, const int32_t* n_nodes,
+                                       const uint64_t* anc_mask, void* out,
+                                       void* workspace, size_t workspace_bytes, void* hip_stream);
 
 /*
  * Tile order for the weights of the skinny projections (an option of fspad_feature_sampler,

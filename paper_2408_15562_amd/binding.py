@@ -33,6 +33,8 @@ EXPORTS = ("fspad_tree_attn_workspace_bytes", "fspad_tree_attn",
            "fspad_draft_layer_workspace_bytes", "fspad_draft_layer", "fspad_packed_weight_bytes", "fspad_pack_weight",
            "fspad_kv_page_bytes", "fspad_page_map", "fspad_kv_store_paged", "fspad_kv_load_paged",
            "fspad_tree_attn_paged_workspace_bytes", "fspad_tree_attn_paged",
+           "fspad_kv_page_bytes_byte", "fspad_kv_store_paged_byte_workspace_bytes", "fspad_kv_store_paged_byte", "fspad_kv_load_paged_byte",
+           "fspad_tree_attn_paged_byte_workspace_bytes", "fspad_tree_attn_paged_byte",
            "fspad_draft_topk_workspace_bytes", "fspad_draft_topk", "fspad_tree_build", "fspad_tree_build_mask",
            "fspad_tree_validate", "fspad_status_string")
 
@@ -138,6 +140,18 @@ def _lib():
         lib.fspad_tree_attn_paged_workspace_bytes.argtypes = [ctypes.POINTER(fspad_paged_desc)]
         lib.fspad_tree_attn_paged.restype = ctypes.c_int
         lib.fspad_tree_attn_paged.argtypes = [ctypes.POINTER(fspad_paged_desc)] + [vp] * 9 + [vp, sz, vp]
+        lib.fspad_kv_page_bytes_byte.restype = sz
+        lib.fspad_kv_page_bytes_byte.argtypes = [i32, i32, i32]
+        lib.fspad_kv_store_paged_byte_workspace_bytes.restype = sz
+        lib.fspad_kv_store_paged_byte_workspace_bytes.argtypes = [ctypes.POINTER(fspad_paged_desc), i32]
+        lib.fspad_kv_store_paged_byte.restype = ctypes.c_int
+        lib.fspad_kv_store_paged_byte.argtypes = [ctypes.POINTER(fspad_paged_desc), i32, vp, vp, i64, i64, vp, vp, vp, sz, vp]
+        lib.fspad_kv_load_paged_byte.restype = ctypes.c_int
+        lib.fspad_kv_load_paged_byte.argtypes = [ctypes.POINTER(fspad_paged_desc), i32, vp, vp, vp, vp, i64, i64, vp]
+        lib.fspad_tree_attn_paged_byte_workspace_bytes.restype = sz
+        lib.fspad_tree_attn_paged_byte_workspace_bytes.argtypes = [ctypes.POINTER(fspad_paged_desc)]
+        lib.fspad_tree_attn_paged_byte.restype = ctypes.c_int
+        lib.fspad_tree_attn_paged_byte.argtypes = [ctypes.POINTER(fspad_paged_desc)] + [vp] * 9 + [vp, sz, vp]
         lib.fspad_draft_topk_workspace_bytes.restype = sz
         lib.fspad_draft_topk_workspace_bytes.argtypes = [i32, i32, i32]
         lib.fspad_draft_topk.restype = ctypes.c_int
@@ -641,29 +655,38 @@ def _on_current_device(*tensors):
             raise ValueError("tensors must live on the current device")
 
 
-def _pool_desc(pages: torch.Tensor, head_dim: int) -> fspad_paged_desc:
-    """Geometry of a pool: uint8 [n_pages, Hkv, page_tokens * D * 17/16], a page's bytes without gaps, pages any stride apart."""
+def _page_tokens(per_head: int, head_dim: int, fp8: bool) -> int:
+    """Tokens of a page from the bytes of one kv head."""
+    if fp8:
+        if head_dim <= 0 or per_head < 16 or (per_head - 16) % (2 * head_dim):
+            raise ValueError("pages must have 2 * page_tokens * head_dim + 16 bytes per kv head")
+        return (per_head - 16) // (2 * head_dim)
+    if head_dim <= 0 or 16 * per_head % (17 * head_dim):
+        raise ValueError("pages must have page_tokens * head_dim * 17/16 bytes per kv head")
+    return 16 * per_head // (17 * head_dim)
+
+
+def _pool_desc(pages: torch.Tensor, head_dim: int, fp8: bool = False) -> fspad_paged_desc:
+    """Geometry of a pool: uint8 [n_pages, Hkv, bytes of a head's part of a page], a page's bytes without gaps, pages any stride apart."""
     if pages.dtype != torch.uint8 or pages.dim() != 3:
         raise ValueError("pages must be a uint8 [n_pages, n_kv_heads, bytes] device tensor")
     n_pages, Hkv, per_head = pages.shape
     if per_head and (pages.stride(2) != 1 or (Hkv > 1 and pages.stride(1) != per_head)):
         raise ValueError("the bytes of a page must be contiguous")
-    if head_dim <= 0 or 16 * per_head % (17 * head_dim):
-        raise ValueError("pages must have page_tokens * head_dim * 17/16 bytes per kv head")
     d = fspad_paged_desc()
     d.batch = d.n_nodes_max = d.n_q_heads = d.table_width = d.table_stride = 1
     d.n_kv_heads, d.head_dim, d.io_dtype, d.out_dtype = Hkv, int(head_dim), FSPAD_BF16, FSPAD_BF16
-    d.page_tokens, d.n_pages = 16 * per_head // (17 * head_dim), n_pages
+    d.page_tokens, d.n_pages = _page_tokens(per_head, head_dim, fp8), n_pages
     d.page_stride = pages.stride(0) if n_pages > 1 else Hkv * per_head
     return d
 
 
 def make_paged_desc(q: torch.Tensor, k_tree: torch.Tensor, pages: torch.Tensor, block_table: torch.Tensor,
                     max_kv_len: Optional[int] = None, out_dtype: Optional[torch.dtype] = None, softmax_scale: float = 0.0,
-                    workgroups: int = 0) -> fspad_paged_desc:
-    """Fill the attention's descriptor from tensor shapes. max_kv_len: what the table's rows can hold, if not given."""
+                    workgroups: int = 0, fp8: bool = False) -> fspad_paged_desc:
+    """Fill the attention's descriptor from tensor shapes. max_kv_len: what the table's rows can hold, if not given. fp8: of 8-bit pages."""
     B, Nmax, Hq, D = q.shape
-    d = _pool_desc(pages, D)
+    d = _pool_desc(pages, D, fp8)
     if pages.shape[1] != k_tree.shape[2]:
         raise ValueError("pages and k_tree must have the same kv heads")
     if block_table.dtype != torch.int32 or block_table.dim() != 2 or block_table.shape[0] != B or block_table.stride(1) != 1:
@@ -696,24 +719,16 @@ def fspad_tree_attn_paged_workspace_bytes(desc: fspad_paged_desc) -> int:
     return int(_lib().fspad_tree_attn_paged_workspace_bytes(ctypes.byref(desc)))
 
 
-def fspad_tree_attn_paged(q: torch.Tensor, k_tree: torch.Tensor, v_tree: torch.Tensor, pages: torch.Tensor,
-                          block_table: torch.Tensor, kv_len: torch.Tensor, n_nodes: torch.Tensor, anc_mask: torch.Tensor,
-                          max_kv_len: Optional[int] = None, out: Optional[torch.Tensor] = None,
-                          workspace: Optional[torch.Tensor] = None, softmax_scale: float = 0.0,
-                          out_dtype: Optional[torch.dtype] = None, stream=None, desc: Optional[fspad_paged_desc] = None,
-                          prepare: bool = False, workgroups: int = 0):
-    """q [B,Nmax,Hq,D]; k_tree,v_tree [B,Nmax,Hkv,D]; pages uint8 [n_pages,Hkv,page bytes per head] (any page stride);
-    block_table int32 [B,width]; kv_len,n_nodes DEVICE int32 [B]; anc_mask device int64/uint64 [B,Nmax]. max_kv_len: no
-    sequence is longer (the launch is laid out for it; what the table's rows hold, if not given). desc: a descriptor from
-    make_paged_desc in the place of max_kv_len, softmax_scale, out_dtype and workgroups; it has to agree with the tensors, and
-    with those arguments where they are given. Returns out [B,Nmax,Hq,D]; with prepare=True a PreparedCall."""
+def _tree_attn_paged(q, k_tree, v_tree, pages, block_table, kv_len, n_nodes, anc_mask, max_kv_len, out, workspace, softmax_scale, out_dtype,
+                     stream, desc, prepare, workgroups, fp8):
     B, Nmax, Hq, D = q.shape
     for name, t, shape in (("q", q, tuple(q.shape)), ("k_tree", k_tree, (B, Nmax, k_tree.shape[2], D)),
                            ("v_tree", v_tree, tuple(k_tree.shape))):
         if not t.is_contiguous() or t.dtype != q.dtype or tuple(t.shape) != shape:
             raise ValueError(f"{name} must be a contiguous {shape} tensor of q's dtype")
     made = make_paged_desc(q, k_tree, pages, block_table, max_kv_len,
-                           out_dtype if out_dtype is not None else (out.dtype if out is not None else None), softmax_scale, workgroups)
+                           out_dtype if out_dtype is not None else (out.dtype if out is not None else None), softmax_scale, workgroups,
+                           fp8)
     if desc is None:
         desc = made
     else:
@@ -733,14 +748,31 @@ def fspad_tree_attn_paged(q: torch.Tensor, k_tree: torch.Tensor, v_tree: torch.T
     if out.dtype != want or not out.is_contiguous() or out.shape != q.shape:
         raise ValueError(f"out must be a contiguous {want} tensor of q's shape")
     if workspace is None:
-        workspace = torch.empty(max(16, fspad_tree_attn_paged_workspace_bytes(desc)), dtype=torch.uint8, device=q.device)
+        size_of = fspad_tree_attn_paged_byte_workspace_bytes if fp8 else fspad_tree_attn_paged_workspace_bytes
+        workspace = torch.empty(max(16, size_of(desc)), dtype=torch.uint8, device=q.device)
     args = (ctypes.byref(desc), _dev_ptr(q, "q"), _dev_ptr(k_tree, "k_tree"), _dev_ptr(v_tree, "v_tree"), _dev_ptr(pages, "pages"),
             _dev_ptr(block_table, "block_table"), _dev_ptr(kv_len, "kv_len"), _dev_ptr(n_nodes, "n_nodes"),
             _dev_ptr(anc_mask, "anc_mask"), _dev_ptr(out, "out"), _dev_ptr(workspace, "workspace"),
             workspace.numel() * workspace.element_size(), _stream_ptr(stream))
     _on_current_device(q, k_tree, v_tree, pages, block_table, kv_len, n_nodes, anc_mask, out, workspace)
     keep = (desc, q, k_tree, v_tree, pages, block_table, kv_len, n_nodes, anc_mask, out, workspace)
-    return _issue(_lib().fspad_tree_attn_paged, "fspad_tree_attn_paged", args, keep, out, prepare)
+    where = "fspad_tree_attn_paged_byte" if fp8 else "fspad_tree_attn_paged"
+    return _issue(getattr(_lib(), where), where, args, keep, out, prepare)
+
+
+def fspad_tree_attn_paged(q: torch.Tensor, k_tree: torch.Tensor, v_tree: torch.Tensor, pages: torch.Tensor,
+                          block_table: torch.Tensor, kv_len: torch.Tensor, n_nodes: torch.Tensor, anc_mask: torch.Tensor,
+                          max_kv_len: Optional[int] = None, out: Optional[torch.Tensor] = None,
+                          workspace: Optional[torch.Tensor] = None, softmax_scale: float = 0.0,
+                          out_dtype: Optional[torch.dtype] = None, stream=None, desc: Optional[fspad_paged_desc] = None,
+                          prepare: bool = False, workgroups: int = 0):
+    """q [B,Nmax,Hq,D]; k_tree,v_tree [B,Nmax,Hkv,D]; pages uint8 [n_pages,Hkv,page bytes per head] (any page stride);
+    block_table int32 [B,width]; kv_len,n_nodes DEVICE int32 [B]; anc_mask device int64/uint64 [B,Nmax]. max_kv_len: no
+    sequence is longer (the launch is laid out for it; what the table's rows hold, if not given). desc: a descriptor from
+    make_paged_desc in the place of max_kv_len, softmax_scale, out_dtype and workgroups; it has to agree with the tensors, and
+    with those arguments where they are given. Returns out [B,Nmax,Hq,D]; with prepare=True a PreparedCall."""
+    return _tree_attn_paged(q, k_tree, v_tree, pages, block_table, kv_len, n_nodes, anc_mask, max_kv_len, out, workspace, softmax_scale, out_dtype,
+                            stream, desc, prepare, workgroups, False)
 
 
 def _paged_rows(k, v, slots):
@@ -771,10 +803,8 @@ def fspad_kv_store_paged(k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, 
     return _issue(_lib().fspad_kv_store_paged, "fspad_kv_store_paged", args, (desc, k, v, slots, pages), pages, prepare)
 
 
-def fspad_kv_load_paged(slots: torch.Tensor, pages: torch.Tensor, head_dim: int, outputs=None, stream=None, prepare: bool = False):
-    """Returns (k, v) bf16 [rows,Hkv,head_dim], rows = slots.numel(): what the slots hold, zeros for slots outside the pool. `outputs`
-    may bring the two tensors, with rows and heads any stride apart (a cache's own, say). With prepare=True a PreparedCall."""
-    desc = _pool_desc(pages, head_dim)
+def _load_paged(slots, pages, head_dim, outputs, stream, prepare, fp8):
+    desc = _pool_desc(pages, head_dim, fp8)
     if outputs is None:
         outputs = tuple(torch.empty((slots.numel(), pages.shape[1], head_dim), dtype=torch.bfloat16, device=pages.device) for _ in range(2))
     k, v = outputs
@@ -784,7 +814,14 @@ def fspad_kv_load_paged(slots: torch.Tensor, pages: torch.Tensor, head_dim: int,
     args = (ctypes.byref(desc), rows, _dev_ptr(slots, "slots"), _dev_ptr(pages, "pages"), _dev_ptr(k, "k"), _dev_ptr(v, "v"), row_stride,
             head_stride, _stream_ptr(stream))
     _on_current_device(k, v, slots, pages)
-    return _issue(_lib().fspad_kv_load_paged, "fspad_kv_load_paged", args, (desc, slots, pages, k, v), (k, v), prepare)
+    where = "fspad_kv_load_paged_byte" if fp8 else "fspad_kv_load_paged"
+    return _issue(getattr(_lib(), where), where, args, (desc, slots, pages, k, v), (k, v), prepare)
+
+
+def fspad_kv_load_paged(slots: torch.Tensor, pages: torch.Tensor, head_dim: int, outputs=None, stream=None, prepare: bool = False):
+    """Returns (k, v) bf16 [rows,Hkv,head_dim], rows = slots.numel(): what the slots hold, zeros for slots outside the pool. `outputs`
+    may bring the two tensors, with rows and heads any stride apart (a cache's own, say). With prepare=True a PreparedCall."""
+    return _load_paged(slots, pages, head_dim, outputs, stream, prepare, False)
 
 
 def fspad_page_map(kv_len: torch.Tensor, n_new: torch.Tensor, block_table: torch.Tensor, free_pages: torch.Tensor,
@@ -821,6 +858,52 @@ def fspad_page_map(kv_len: torch.Tensor, n_new: torch.Tensor, block_table: torch
     _on_current_device(kv_len, n_new, path, block_table, free_pages, n_free, *outputs)
     keep = (kv_len, n_new, path, block_table, free_pages, n_free)
     return _issue(_lib().fspad_page_map, "fspad_page_map", args, keep, outputs, prepare)
+
+
+# ---- paged 8-bit cache (the format is in include/fspad.h)
+
+def fspad_kv_page_bytes_byte(n_kv_heads: int, head_dim: int, page_tokens: int) -> int:
+    return int(_lib().fspad_kv_page_bytes_byte(int(n_kv_heads), int(head_dim), int(page_tokens)))
+
+
+def fspad_tree_attn_paged_byte_workspace_bytes(desc: fspad_paged_desc) -> int:
+    return int(_lib().fspad_tree_attn_paged_byte_workspace_bytes(ctypes.byref(desc)))
+
+
+def fspad_tree_attn_paged_byte(q: torch.Tensor, k_tree: torch.Tensor, v_tree: torch.Tensor, pages: torch.Tensor,
+                               block_table: torch.Tensor, kv_len: torch.Tensor, n_nodes: torch.Tensor, anc_mask: torch.Tensor,
+                               max_kv_len: Optional[int] = None, out: Optional[torch.Tensor] = None,
+                               workspace: Optional[torch.Tensor] = None, softmax_scale: float = 0.0,
+                               out_dtype: Optional[torch.dtype] = None, stream=None, desc: Optional[fspad_paged_desc] = None,
+                               prepare: bool = False, workgroups: int = 0):
+    """fspad_tree_attn_paged over 8-bit pages (a descriptor from make_paged_desc is one made with fp8=True)."""
+    return _tree_attn_paged(q, k_tree, v_tree, pages, block_table, kv_len, n_nodes, anc_mask, max_kv_len, out, workspace, softmax_scale, out_dtype,
+                            stream, desc, prepare, workgroups, True)
+
+
+def fspad_kv_store_paged_byte_workspace_bytes(desc: fspad_paged_desc, rows: int) -> int:
+    return int(_lib().fspad_kv_store_paged_byte_workspace_bytes(ctypes.byref(desc), int(rows)))
+
+
+def fspad_kv_store_paged_byte(k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, pages: torch.Tensor, workspace: Optional[torch.Tensor] = None,
+                             stream=None, prepare: bool = False):
+    """fspad_kv_store_paged into 8-bit pages. A call that stores the first token of a block of 32 begins the block; to other blocks it
+    adds. `workspace`: 4 bytes a slot of the pool, for more than 1024 rows. Returns pages; with prepare=True a PreparedCall."""
+    rows, Hkv, D, (row_stride, head_stride) = _paged_rows(k, v, slots)
+    desc = _pool_desc(pages, D, fp8=True)
+    if pages.shape[1] != Hkv:
+        raise ValueError("pages must have the kv heads of k and v")
+    if workspace is None:
+        workspace = torch.empty(max(16, fspad_kv_store_paged_byte_workspace_bytes(desc, rows)), dtype=torch.uint8, device=pages.device)
+    args = (ctypes.byref(desc), rows, _dev_ptr(k, "k"), _dev_ptr(v, "v"), row_stride, head_stride, _dev_ptr(slots, "slots"),
+            _dev_ptr(pages, "pages"), _dev_ptr(workspace, "workspace"), workspace.numel() * workspace.element_size(), _stream_ptr(stream))
+    _on_current_device(k, v, slots, pages, workspace)
+    return _issue(_lib().fspad_kv_store_paged_byte, "fspad_kv_store_paged_byte", args, (desc, k, v, slots, pages, workspace), pages, prepare)
+
+
+def fspad_kv_load_paged_byte(slots: torch.Tensor, pages: torch.Tensor, head_dim: int, outputs=None, stream=None, prepare: bool = False):
+    """fspad_kv_load_paged from 8-bit pages."""
+    return _load_paged(slots, pages, head_dim, outputs, stream, prepare, True)
 
 
 def fspad_draft_topk_workspace_bytes(rows: int, V: int, k: int) -> int:

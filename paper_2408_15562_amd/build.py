@@ -14,8 +14,8 @@ ROOFS_LIB_PATH = os.path.join(_HERE, "libfspad_roofs.so")   # the benchmark's me
 LATE_LIB_PATH = os.path.join(_HERE, "libfspad_late.so")
 OBJ_DIR = os.path.join(_HERE, "_build")
 SOURCES = ["fspad_host.cpp", "fspad_attn.hip", "fspad_accept.hip", "fspad_commit.hip", "fspad_tree.hip", "fspad_lmhead.hip",
-           "fspad_topk.hip", "fspad_draft.hip", "fspad_paged.hip", "fspad_attn_paged.hip"]
-HEADERS = ["attn_plan.h", "greedy_walk.h", "stream_gemm.h", "exp_nonpos.h", "paged_forms.h", "paged_layout.h", "paged_plan.h", "wave_scan.h"]
+           "fspad_topk.hip", "fspad_draft.hip", "fspad_paged.hip", "fspad_attn_paged.hip", "fspad_paged_fp8.hip", "fspad_attn_paged_fp8.hip"]
+HEADERS = ["attn_plan.h", "greedy_walk.h", "stream_gemm.h", "exp_nonpos.h", "paged_attn.h", "paged_forms.h", "paged_forms_fp8.h", "paged_layout.h", "paged_plan.h", "wave_scan.h"]
 
 _FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
           # packed fp32 VALU ops are kept off on the test machines
@@ -26,7 +26,7 @@ _FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
 # per-source options. The attention kernels keep the results of their matrix instructions in ordinary
 # vector registers: left to itself the compiler puts the score tiles into accumulation registers and
 # copies every one of them out again for the softmax (a quarter of the instructions of a block).
-EXTRA_FLAGS = {src: ["-mllvm", "-amdgpu-mfma-vgpr-form=1"] for src in ("fspad_attn.hip", "fspad_attn_paged.hip")}
+EXTRA_FLAGS = {src: ["-mllvm", "-amdgpu-mfma-vgpr-form=1"] for src in ("fspad_attn.hip", "fspad_attn_paged.hip", "fspad_attn_paged_fp8.hip")}
 
 
 def compile_command(src: str, obj: str, defines=()):

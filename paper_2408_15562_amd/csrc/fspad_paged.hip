@@ -151,7 +151,7 @@ fspad_status move_rows(bool store, const fspad_paged_desc* desc, int32_t rows, v
                        int64_t head_stride, const int32_t* slots, void* pages, void* hip_stream) {
   if (!desc) return FSPAD_ERR_NULL;
   const fspad_paged_desc& d = *desc;
-  if (const fspad_status st = check_pool(d)) return st;
+  if (const fspad_status st = check_pool(d, PagedFormat::kFp4)) return st;
   if (rows < 0 || d.n_kv_heads > 65535) return FSPAD_ERR_SHAPE;
   if (rows == 0) return FSPAD_OK;
   if (!k || !v || !slots || !pages) return FSPAD_ERR_NULL;

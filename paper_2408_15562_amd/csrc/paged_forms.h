@@ -1,5 +1,6 @@
 // The two forms of a wavefront's work in the attention over a paged 4-bit cache: what its lanes hold of a 32-key block and of its
-// query rows, and the products. Internal to the library. gfx950 (CDNA4) only.
+// query rows, and the products. What an 8-bit cache's blocks change of them is in paged_forms_fp8.h (PLAIN: channels and keys in the order of
+// its pages). Internal to the library. gfx950 (CDNA4) only.
 //
 // Form16: 16 query rows, on 16x16 products (one token of up to 16 heads, small trees). Form32: tiles of 32 rows, on 32x32 ones, which leave
 // the other wavefront of a SIMD more room: beside a stream of 16x16x32 bf16 products one of its vector instructions takes 8.5 clocks,
@@ -110,21 +111,23 @@ struct BlockPlace {
 //        two products (hi, lo); D = 64 in one, K's 64 channels twice in its 128.
 //   O^T: v_mfma_f32_16x16x32_bf16: D/16 channels of keys 4 g4 .. 4 g4 + 3 and 16 more, bf16 by v_cvt_scalef32_pk_bf16_fp4 (V's scales run along
 //        the channels, not along the keys that are summed over), turned from key to channel order two bytes at a time.
-template <int D>
+template <int D, bool PLAIN = false>
 struct Form16 {
   static constexpr int HEAD_DIM = D, TILE = 16, RT = 1, ROWS = 16, NX = 8, E = D / 16, KS = D / 32;
   static constexpr int QUADS = D / 16;   // quads of channels of a row that a lane holds
 
   __device__ static __forceinline__ int row(int lane) { return lane & 15; }
-  __device__ static __forceinline__ int first_key(int lane) { return 4 * (lane >> 4); }
-  __device__ static constexpr int key_of(int j) { return (j & 3) + 16 * (j >> 2); }   // less the lane's first
+  __device__ static __forceinline__ int first_key(int lane) { return (PLAIN ? 8 : 4) * (lane >> 4); }
+  __device__ static constexpr int key_of(int j) { return PLAIN ? j : (j & 3) + 16 * (j >> 2); }   // less the lane's first
+  // the key that row m of the products' operand kt is
+  __device__ static __forceinline__ int operand_key(int kt, int m) { return PLAIN ? 8 * (m >> 2) + 4 * kt + (m & 3) : 16 * kt + m; }
   __device__ static __forceinline__ float row_max(float x) {
     x = fmaxf(x, __shfl_xor(x, 16));
     return fmaxf(x, __shfl_xor(x, 32));
   }
 
   struct State {
-    f32x4 o[E];   // entry i <-> channel E (4 g4 + i) + e
+    f32x4 o[E];   // entry i <-> channel E (4 g4 + i) + e; PLAIN: with KS sums of each half of the channels, KS (16 (e / KS) + 4 g4 + i) + e % KS
     float m[RT], l[RT];
   };
   __device__ static __forceinline__ void clear(State& st, float m) {
@@ -141,10 +144,17 @@ struct Form16 {
   __device__ static __forceinline__ float row_sum(const State& st, int) { return st.l[0]; }
   // quad q: four channels from channel(q, lane) on
   __device__ static __forceinline__ f32x4 quad(const State& st, int, int q) {
+    if constexpr (PLAIN && D == 64) {   // (two entries' channels follow one another)
+      const int i = 2 * (q & 1), e = 2 * (q >> 1);
+      return f32x4{st.o[e][i], st.o[e + 1][i], st.o[e][i + 1], st.o[e + 1][i + 1]};
+    }
     const int i = q & 3, e = 4 * (q >> 2);
     return f32x4{st.o[e][i], st.o[e + 1][i], st.o[e + 2][i], st.o[e + 3][i]};
   }
-  __device__ static __forceinline__ int channel(int q, int lane) { return E * (4 * (lane >> 4) + (q & 3)) + 4 * (q >> 2); }
+  __device__ static __forceinline__ int channel(int q, int lane) {
+    if constexpr (PLAIN) return D == 64 ? 2 * (16 * (q >> 1) + 4 * (lane >> 4) + 2 * (q & 1)) : 4 * (16 * (q >> 2) + 4 * (lane >> 4) + (q & 3));
+    else return E * (4 * (lane >> 4) + (q & 3)) + 4 * (q >> 2);
+  }
 
   // ---- query rows: 16-byte pieces of a row, as the tree's products take them one by one
   static constexpr int PIECES = D / 32;
@@ -181,6 +191,10 @@ struct Form16 {
   struct Values {
     unsigned c[D / 16], scale[2];
   };
+  // where a block's codes and scales start in a head's part of a page, in which a lane's Offsets are counted
+  __device__ static constexpr int head_bytes(int P) { return page_head_bytes(D, P); }
+  __device__ static __forceinline__ unsigned block_codes(unsigned in_page) { return in_page * (D / 2); }
+  __device__ static __forceinline__ unsigned block_scales(unsigned in_page) { return in_page; }
   struct Offsets { unsigned k, ks, v, vs; };
   template <bool WIDE>
   __device__ static __forceinline__ Offsets offsets(int lane, int P) {
@@ -240,12 +254,15 @@ struct Form16 {
       for (int i = 0; i < 4; ++i) s[0][4 * kt + i] = r[i];
     }
   }
-  template <typename PairFn, typename HalfFn>
-  __device__ static __forceinline__ void add(State& st, const u32x4 (&w)[RT][1], PairFn&& pairs, HalfFn&& halfway) {
+  __device__ static __forceinline__ void add_weights(State& st, const u32x4 (&w)[RT][1]) {
     bf16x8 ones;
 #pragma unroll
     for (int j = 0; j < 8; ++j) ones[j] = (__bf16)1.0f;
     st.l[0] += __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, __builtin_bit_cast(bf16x8, w[0][0]), f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0)[0];   // (all entries equal)
+  }
+  template <typename PairFn, typename HalfFn>
+  __device__ static __forceinline__ void add(State& st, const u32x4 (&w)[RT][1], PairFn&& pairs, HalfFn&& halfway) {
+    add_weights(st, w);
 #pragma unroll
     for (int e2 = 0; e2 < E / 2; ++e2) {
       if (e2 == E / 4) halfway();
@@ -279,13 +296,27 @@ struct Form16 {
   __device__ static __forceinline__ void load_tree(TreeKeys& k, TreeValues& v, const char* kr, const char* vr, int64_t row_bytes, int t0, int last, int lane) {
 #pragma unroll
     for (int kt = 0; kt < 2; ++kt) {
-      const char* src = kr + min(t0 + 16 * kt + (lane & 15), last) * row_bytes;
+      const char* src = kr + min(t0 + operand_key(kt, lane & 15), last) * row_bytes;
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) k.k[kt][ks] = *reinterpret_cast<const bf16x8*>(src + 2 * piece_channel(ks, lane));
     }
 #pragma unroll
     for (int j = 0; j < NX; ++j) {
-      const char* src = vr + min(t0 + first_key(lane) + key_of(j), last) * row_bytes + 2 * E * (lane & 15);
+      const char* row = vr + min(t0 + first_key(lane) + key_of(j), last) * row_bytes;
+      if constexpr (PLAIN) {   // of each half of the channels the lane's KS
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const char* src = row + 2 * (D / 2 * i + KS * (lane & 15));
+          if constexpr (D == 128) {
+            const u32x2 w = *reinterpret_cast<const u32x2*>(src);
+            v.v[j][2 * i] = w[0]; v.v[j][2 * i + 1] = w[1];
+          } else {
+            v.v[j][i] = *reinterpret_cast<const unsigned*>(src);
+          }
+        }
+        continue;
+      }
+      const char* src = row + 2 * E * (lane & 15);
       if constexpr (D == 128) {
         const u32x4 w = *reinterpret_cast<const u32x4*>(src);
 #pragma unroll
@@ -314,13 +345,17 @@ struct Form16 {
   }
   // the weight of a key of the block for the lane's row
   __device__ static __forceinline__ float weight_of(const u32x4 (&w)[1], int key, int lane) {
+    const int at = PLAIN ? key & 7 : (key & 3) + 4 * (key >> 4);
     float own = 0.f;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) own = (key & 3) + 4 * (key >> 4) == j ? bf16_at(w[0][j >> 1], j & 1) : own;
-    return __shfl(own, 16 * ((key >> 2) & 3) + (lane & 15));
+    for (int j = 0; j < 8; ++j) own = at == j ? bf16_at(w[0][j >> 1], j & 1) : own;
+    return __shfl(own, 16 * (PLAIN ? key >> 3 : (key >> 2) & 3) + (lane & 15));
   }
   // add(q, k, x): the sums of channel channel(q) + k get x
-  __device__ static __forceinline__ void add_to(State& st, int, int q, int k, float x) { st.o[4 * (q >> 2) + k][q & 3] += x; }
+  __device__ static __forceinline__ void add_to(State& st, int, int q, int k, float x) {
+    if constexpr (PLAIN && D == 64) st.o[2 * (q >> 1) + (k & 1)][2 * (q & 1) + (k >> 1)] += x;
+    else st.o[4 * (q >> 2) + k][q & 3] += x;
+  }
 };
 
 // ---------------------------------------------------------------------------------------------------------------------------
@@ -330,7 +365,7 @@ struct Form16 {
 //        Lanes col and col + 16 share runs: each loads eight of the keys and gives the other its half of them
 //        (v_permlane16_swap_b32), instead of both loading all 16.
 //   Row sums: v_mfma_f32_4x4x4_16b_bf16 with ones adds a lane's own weights four at a time; the halves of a row meet at the end.
-template <int D, int TILES>
+template <int D, int TILES, bool PLAIN = false>
 struct Form32 {
   static constexpr int HEAD_DIM = D, TILE = 32, RT = TILES, ROWS = 32 * TILES, NX = 16, E = D / 32, KB = D / 64;
   static constexpr int QUADS = D / 8;
@@ -364,16 +399,21 @@ struct Form32 {
     for (int e = 0; e < E; ++e) st.o[t][e] *= a;
   }
   __device__ static __forceinline__ float row_sum(const State& st, int t) { return st.l[t][0] + __shfl_xor(st.l[t][0], 32); }
-  // D = 128: quad q is entry q of the four tiles. D = 64: entries q and q + 8 of the two (q < 8), whose channels follow one another.
+  // D = 128: quad q is entry q of the four tiles. D = 64: entries q and q + 8 of the two (q < 8), or 2 q and 2 q + 1, whose channels follow one another.
   __device__ static __forceinline__ f32x4 quad(const State& st, int t, int q) {
     if constexpr (D == 128) return f32x4{st.o[t][0][q], st.o[t][1][q], st.o[t][E - 2][q], st.o[t][E - 1][q]};
+    else if constexpr (PLAIN) return f32x4{st.o[t][0][2 * q], st.o[t][1][2 * q], st.o[t][0][2 * q + 1], st.o[t][1][2 * q + 1]};
     else return f32x4{st.o[t][0][q], st.o[t][1][q], st.o[t][0][q + 8], st.o[t][1][q + 8]};
   }
   // first channel of a lane of V: 2 E channels a run, E of them the lane's
-  __device__ static constexpr int values_channel(int col) { return 2 * E * (col & 15) + E * (col >> 4); }
-  __device__ static __forceinline__ int channel(int q, int lane) { return values_channel(8 * (q >> 2) + 4 * (lane >> 5) + (q & 3)); }
+  __device__ static constexpr int values_channel(int col) { return PLAIN ? E * col : 2 * E * (col & 15) + E * (col >> 4); }
+  __device__ static __forceinline__ int channel(int q, int lane) {
+    const int r = PLAIN && D == 64 ? 2 * q : q;
+    return values_channel(8 * (r >> 2) + 4 * (lane >> 5) + (r & 3));
+  }
   __device__ static __forceinline__ void add_to(State& st, int t, int q, int k, float x) {
     if constexpr (D == 128) st.o[t][k][q] += x;
+    else if constexpr (PLAIN) st.o[t][k & 1][2 * q + (k >> 1)] += x;
     else st.o[t][k & 1][q + 8 * (k >> 1)] += x;
   }
 
@@ -403,6 +443,10 @@ struct Form32 {
   struct Values {
     unsigned c[4 * KB], scale[4];   // eight of the lane's 16 keys, the scales of all
   };
+  // where a block's codes and scales start in a head's part of a page, in which a lane's Offsets are counted
+  __device__ static constexpr int head_bytes(int P) { return page_head_bytes(D, P); }
+  __device__ static __forceinline__ unsigned block_codes(unsigned in_page) { return in_page * (D / 2); }
+  __device__ static __forceinline__ unsigned block_scales(unsigned in_page) { return in_page; }
   struct Offsets { unsigned k, ks, v, vs; };
   template <bool WIDE>
   __device__ static __forceinline__ Offsets offsets(int lane, int P) {

@@ -38,7 +38,7 @@ inline int64_t paged_unit_blocks(const fspad_paged_desc& d) {   // at most
 // D = 64, two slabs of 32 with D = 128, whose wavefronts read the same keys. Four wavefronts or eight, by the rules below. A piece starts and ends
 // in 8 us, pieces are joined in 5 us, and a wavefront takes 0.3 us a block when the device is full: the costs below. What is known of the lengths here
 // is max_kv_len alone.
-inline PagedPlan plan_paged(const fspad_paged_desc& d) {
+inline PagedPlan plan_paged(const fspad_paged_desc& d, PagedFormat = PagedFormat::kFp4) {
   PagedPlan pl{};
   const int rows = d.n_nodes_max * (d.n_q_heads / d.n_kv_heads);
   pl.rows_per_group = rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
@@ -80,8 +80,8 @@ inline PagedPlan plan_paged(const fspad_paged_desc& d) {
   return pl;
 }
 
-inline fspad_status check_paged_attn(const fspad_paged_desc& d) {
-  if (const fspad_status st = check_pool(d)) return st;
+inline fspad_status check_paged_attn(const fspad_paged_desc& d, PagedFormat format = PagedFormat::kFp4) {
+  if (const fspad_status st = check_pool(d, format)) return st;
   if (d.batch < 1 || d.batch > kPagedMaxBatch || d.n_nodes_max < 1 || d.n_nodes_max > FSPAD_MAX_NODES) return FSPAD_ERR_SHAPE;
   if (d.n_q_heads < 1 || d.n_q_heads % d.n_kv_heads != 0) return FSPAD_ERR_SHAPE;
   if (d.out_dtype != FSPAD_BF16 && d.out_dtype != FSPAD_F32) return FSPAD_ERR_DTYPE;
@@ -91,7 +91,7 @@ inline fspad_status check_paged_attn(const fspad_paged_desc& d) {
   // 32-bit rows, units and blocks of all units, and launch dimensions
   const int64_t rows = (int64_t)d.n_nodes_max * (d.n_q_heads / d.n_kv_heads);
   if (rows > (1 << 20) || d.n_kv_heads > 65535) return FSPAD_ERR_SHAPE;
-  const PagedPlan pl = plan_paged(d);
+  const PagedPlan pl = plan_paged(d, format);
   if ((int64_t)d.batch * pl.groups > 65535) return FSPAD_ERR_SHAPE;
   if ((int64_t)d.batch * d.n_kv_heads * pl.groups * paged_unit_blocks(d) > (1 << 30)) return FSPAD_ERR_SHAPE;
   return FSPAD_OK;

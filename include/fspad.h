@@ -28,7 +28,9 @@
  *      fspad_draft_topk, fspad_tree_build);
  *   6. the same attention over a paged 4-bit cache, with the calls that keep it (fspad_tree_attn_paged,
  *      fspad_page_map, fspad_kv_store_paged, fspad_kv_load_paged), and over a paged 8-bit one
- *      (fspad_tree_attn_paged_byte, fspad_kv_store_paged_byte, fspad_kv_load_paged_byte).
+ *      (fspad_tree_attn_paged_byte, fspad_kv_store_paged_byte, fspad_kv_load_paged_byte);
+ *   7. sequences that share pages of either: fspad_page_fork, fspad_page_release, fspad_page_compact,
+ *      fspad_page_copy.
  *
  * Conventions that hold for every entry point:
  *   - "dev" pointers are device (HBM) addresses, "host" pointers are host
@@ -568,6 +570,85 @@ fspad_status fspad_tree_attn_paged_byte(const fspad_paged_desc* desc,
                                        const int32_t* kv_len, const int32_t* n_nodes,
                                        const uint64_t* anc_mask, void* out,
                                        void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * Shared pages (no passage of the paper: several continuations of one prompt hold its pages once). Beside the block tables, lengths and stack of
+ * fspad_page_map there is an array shared [n_pages] i32: how many sequences hold a page beside the first, 0 for pages that one holds or none
+ * (counts below zero are taken as 0). It starts as zeros; fspad_page_map neither reads nor changes it, since pages that it gives are new. Sequences of whose pages
+ * any may be shared end by fspad_page_release, not by n_new < 0. Only full pages are ever shared, so that growth writes to pages of a
+ * sequence's own. The calls are about block tables: they serve the 4-bit and the 8-bit cache alike, all layers at once.
+ *
+ *   B           rows of the block table, 1..2048;  page_tokens 16, 32, 64, 128 or 256;  n_pages 1..2^20 (n_pages and table_width times page_tokens <= 2^31 - 1)
+ *   block_table dev [B] rows of table_width i32, table_stride entries apart (B * table_width <= 2^30)
+ *   kv_len      dev [B] i32 (negative lengths count as 0); sequence b holds the first ceil(kv_len[b] / P) entries of its row
+ *   free_pages  dev [n_pages] i32, n_free dev [1] i32 (taken as 0..n_pages): the stack of fspad_page_map. It names no page twice and none that is held
+ *   outputs     kv_len_out may be kv_len, n_free_out n_free, shared_out shared; else they do not overlap with inputs
+ * Entries of tables and of the stack outside [0,n_pages) count for no page. None of the calls allocates or synchronises; results are the same from run to run.
+ */
+
+/*
+ * Forks: for f < n_forks in order, row dst[f] becomes the first n_tokens[f] tokens of row src[f] (all lengths before the call).
+ *   full pages   the first n_tokens[f] / P entries of row src[f], which both rows hold from now on: each page's count goes up by one for each fork
+ *   the rest     n_tokens[f] % P tokens, if there are any, go to a page off the top of the stack: copy_src[f] = the page in row src[f], copy_dst[f] = the new
+ *                one, for fspad_page_copy in every layer's pool, before the row is read or stored to
+ * granted[f] = 1 and kv_len_out[dst[f]] = n_tokens[f]; lengths of other rows are those before the call. copy_src[f] = copy_dst[f] = -1 where nothing is to be copied.
+ * A fork is refused, granted[f] = 0 with nothing changed for it, if src[f] or dst[f] is outside [0,B), or they are the same, if row dst[f] has tokens or a fork
+ * before f in the call names it too (refused or not), if n_tokens[f] is below zero, above kv_len[src[f]], or more than a row holds, or if it needs a page and there
+ * are as many forks before it that need one (refused for lack of pages or not, but not those refused for another reason) as the stack has.
+ *   n_forks     1..2048;  src, dst dev [n_forks] i32;  n_tokens dev [n_forks] i32, NULL: all tokens of src
+ *   copy_src, copy_dst, granted   dev [n_forks] i32 out;  n_free_out dev [1] out;  shared_out dev [n_pages] out
+ * No workspace. The stack itself is not written to.
+ */
+fspad_status fspad_page_fork(int32_t B, int32_t page_tokens, int32_t n_pages, int32_t table_width, int64_t table_stride, int32_t n_forks,
+                             const int32_t* src, const int32_t* dst, const int32_t* n_tokens, const int32_t* kv_len,
+                             int32_t* block_table, const int32_t* free_pages, const int32_t* n_free, const int32_t* shared,
+                             int32_t* copy_src, int32_t* copy_dst, int32_t* kv_len_out, int32_t* n_free_out,
+                             int32_t* shared_out, int32_t* granted, void* hip_stream);
+
+/*
+ * Ends: sequences b with ended[b] != 0 give up the pages they hold, kv_len_out[b] = 0 (others keep their lengths). A page that more of them hold than its
+ * count says is held by nobody then: it goes onto the stack, with a count of 0, the pages of a call in ascending order. Counts of others go down by the
+ * sequences that held them. Rows of the table keep their entries.
+ *   ended       dev [B] i32;  free_pages is written behind the first n_free entries
+ *   workspace   dev, 16-byte aligned, >= fspad_page_release_workspace_bytes(B, n_pages, table_width) (0 for small calls: may be NULL then);
+ *               contents ignored on entry, undefined on exit; two calls that may overlap in time need different ones
+ */
+size_t fspad_page_release_workspace_bytes(int32_t B, int32_t n_pages, int32_t table_width);
+
+fspad_status fspad_page_release(int32_t B, int32_t page_tokens, int32_t n_pages, int32_t table_width, int64_t table_stride,
+                                const int32_t* ended, const int32_t* kv_len, const int32_t* block_table,
+                                int32_t* free_pages, const int32_t* n_free, const int32_t* shared,
+                                int32_t* kv_len_out, int32_t* n_free_out, int32_t* shared_out,
+                                void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * Compaction: what is held moves to the first keep = n_pages - n_free pages of the pool, so that the rest of it can be given back (or a larger pool begin).
+ * Pages from keep on that are not on the stack go to the pages before keep that are, both in ascending order. copy_src[i], copy_dst[i] are the moves, in this order, -1
+ * behind the last one: for fspad_page_copy in every layer's pool, before it is read or stored to. Held entries of the tables and counts follow their
+ * pages; the stack is n_pages - 1, n_pages - 2, .. keep, its height what it was, -1 behind.
+ *   copy_src, copy_dst   dev [n_pages / 2] i32 out (may be NULL if n_pages is 1)
+ *   block_table_out      dev [B] rows of table_width i32, out_stride entries apart: may be block_table (with its stride); else entries that are not held are copied
+ *   free_out, shared_out dev [n_pages] i32 out: may be free_pages and shared
+ *   workspace   dev, 16-byte aligned, >= fspad_page_compact_workspace_bytes(n_pages); contents ignored on entry, undefined on exit; two calls
+ *               that may overlap in time need different ones
+ */
+size_t fspad_page_compact_workspace_bytes(int32_t n_pages);
+
+fspad_status fspad_page_compact(int32_t B, int32_t page_tokens, int32_t n_pages, int32_t table_width, int64_t table_stride, int64_t out_stride,
+                                const int32_t* kv_len, const int32_t* block_table, const int32_t* free_pages,
+                                const int32_t* n_free, const int32_t* shared, int32_t* copy_src, int32_t* copy_dst,
+                                int32_t* block_table_out, int32_t* free_out, int32_t* shared_out,
+                                void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * Copies: page copy_dst[i] of a pool becomes what page copy_src[i] is, for i < n_copies where both lie in [0,n_pages) (other pairs are passed over). No
+ * page that is written may stand in another pair of the call.
+ *   pages       dev, 16-byte aligned; n_pages >= 1 pages of page_bytes, page_stride bytes apart (both multiples of 16, page_bytes <= 2^31 - 1, page_stride below 2^32):
+ *               of interleaved pools of several layers, page_bytes may be all of them
+ *   n_copies    >= 0; copy_src, copy_dst dev [n_copies] i32 (0: no pointer is looked at)
+ */
+fspad_status fspad_page_copy(void* pages, int32_t n_pages, int64_t page_stride, int64_t page_bytes, int32_t n_copies,
+                             const int32_t* copy_src, const int32_t* copy_dst, void* hip_stream);
 
 /*
  * Tile order for the weights of the skinny projections (an option of fspad_feature_sampler,

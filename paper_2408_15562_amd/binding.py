@@ -35,6 +35,8 @@ EXPORTS = ("fspad_tree_attn_workspace_bytes", "fspad_tree_attn",
            "fspad_tree_attn_paged_workspace_bytes", "fspad_tree_attn_paged",
            "fspad_kv_page_bytes_byte", "fspad_kv_store_paged_byte_workspace_bytes", "fspad_kv_store_paged_byte", "fspad_kv_load_paged_byte",
            "fspad_tree_attn_paged_byte_workspace_bytes", "fspad_tree_attn_paged_byte",
+           "fspad_page_fork", "fspad_page_release_workspace_bytes", "fspad_page_release", "fspad_page_compact_workspace_bytes", "fspad_page_compact",
+           "fspad_page_copy",
            "fspad_draft_topk_workspace_bytes", "fspad_draft_topk", "fspad_tree_build", "fspad_tree_build_mask",
            "fspad_tree_validate", "fspad_status_string")
 
@@ -152,6 +154,18 @@ def _lib():
         lib.fspad_tree_attn_paged_byte_workspace_bytes.argtypes = [ctypes.POINTER(fspad_paged_desc)]
         lib.fspad_tree_attn_paged_byte.restype = ctypes.c_int
         lib.fspad_tree_attn_paged_byte.argtypes = [ctypes.POINTER(fspad_paged_desc)] + [vp] * 9 + [vp, sz, vp]
+        lib.fspad_page_fork.restype = ctypes.c_int
+        lib.fspad_page_fork.argtypes = [i32, i32, i32, i32, i64, i32] + [vp] * 15
+        lib.fspad_page_release_workspace_bytes.restype = sz
+        lib.fspad_page_release_workspace_bytes.argtypes = [i32, i32, i32]
+        lib.fspad_page_release.restype = ctypes.c_int
+        lib.fspad_page_release.argtypes = [i32, i32, i32, i32, i64] + [vp] * 9 + [vp, sz, vp]
+        lib.fspad_page_compact_workspace_bytes.restype = sz
+        lib.fspad_page_compact_workspace_bytes.argtypes = [i32]
+        lib.fspad_page_compact.restype = ctypes.c_int
+        lib.fspad_page_compact.argtypes = [i32, i32, i32, i32, i64, i64] + [vp] * 10 + [vp, sz, vp]
+        lib.fspad_page_copy.restype = ctypes.c_int
+        lib.fspad_page_copy.argtypes = [vp, i32, i64, i64, i32, vp, vp, vp]
         lib.fspad_draft_topk_workspace_bytes.restype = sz
         lib.fspad_draft_topk_workspace_bytes.argtypes = [i32, i32, i32]
         lib.fspad_draft_topk.restype = ctypes.c_int
@@ -904,6 +918,123 @@ def fspad_kv_store_paged_byte(k: torch.Tensor, v: torch.Tensor, slots: torch.Ten
 def fspad_kv_load_paged_byte(slots: torch.Tensor, pages: torch.Tensor, head_dim: int, outputs=None, stream=None, prepare: bool = False):
     """fspad_kv_load_paged from 8-bit pages."""
     return _load_paged(slots, pages, head_dim, outputs, stream, prepare, True)
+
+
+# ---- pages that several sequences hold
+
+def _check_table(block_table: torch.Tensor, B: int, name: str = "block_table"):
+    if block_table.dtype != torch.int32 or block_table.dim() != 2 or block_table.shape[0] != B or block_table.stride(1) != 1:
+        raise ValueError(f"{name} must be an int32 [B, width] device tensor with contiguous rows")
+
+
+def _check_i32(shapes):
+    for name, t, shape in shapes:
+        if t.dtype != torch.int32 or not t.is_contiguous() or tuple(t.shape) != shape:
+            raise ValueError(f"{name} must be a contiguous int32 {shape} device tensor")
+
+
+def _row_stride(table: torch.Tensor) -> int:
+    return table.stride(0) if table.shape[0] > 1 else table.shape[1]   # (of one row the stride says nothing)
+
+
+def _empty_i32(device, *shapes):
+    return tuple(torch.empty(shape, dtype=torch.int32, device=device) for shape in shapes)
+
+
+def fspad_page_fork(src: torch.Tensor, dst: torch.Tensor, kv_len: torch.Tensor, block_table: torch.Tensor, free_pages: torch.Tensor,
+                    n_free: torch.Tensor, shared: torch.Tensor, page_tokens: int, n_tokens: Optional[torch.Tensor] = None, outputs=None,
+                    stream=None, prepare: bool = False):
+    """Device int32 tensors: src, dst [F] rows of block_table [B,width] (written), n_tokens [F] or None (all of src), kv_len [B], free_pages
+    [n_pages] (the stack), n_free [1], shared [n_pages] (holders of a page beside the first). Returns (copy_src [F], copy_dst [F], kv_len_out [B], n_free_out [1], shared_out
+    [n_pages], granted [F]); `outputs` may bring them (kv_len, n_free and shared themselves as the third to fifth: updated in place). With prepare=True a
+    PreparedCall. fspad_page_copy(copy_src, copy_dst, pages) of every pool belongs behind it."""
+    B, F, n_pages = kv_len.numel(), src.numel(), free_pages.numel()
+    _check_table(block_table, B)
+    if outputs is None:
+        outputs = _empty_i32(kv_len.device, (F,), (F,), (B,), (1,), (n_pages,), (F,))
+    copy_src, copy_dst, kv_len_out, n_free_out, shared_out, granted = outputs
+    _check_i32([("src", src, (F,)), ("dst", dst, (F,)), ("kv_len", kv_len, (B,)), ("free_pages", free_pages, (n_pages,)), ("n_free", n_free, (1,)),
+                ("shared", shared, (n_pages,)), ("copy_src", copy_src, (F,)), ("copy_dst", copy_dst, (F,)), ("kv_len_out", kv_len_out, (B,)),
+                ("n_free_out", n_free_out, (1,)), ("shared_out", shared_out, (n_pages,)), ("granted", granted, (F,))]
+               + ([("n_tokens", n_tokens, (F,))] if n_tokens is not None else []))
+    args = (B, int(page_tokens), n_pages, block_table.shape[1], _row_stride(block_table), F, _dev_ptr(src, "src"), _dev_ptr(dst, "dst"),
+            _dev_ptr(n_tokens, "n_tokens"), _dev_ptr(kv_len, "kv_len"), _dev_ptr(block_table, "block_table"), _dev_ptr(free_pages, "free_pages"),
+            _dev_ptr(n_free, "n_free"), _dev_ptr(shared, "shared"), *(_dev_ptr(t, "outputs") for t in outputs), _stream_ptr(stream))
+    _on_current_device(src, dst, n_tokens, kv_len, block_table, free_pages, n_free, shared, *outputs)
+    keep = (src, dst, n_tokens, kv_len, block_table, free_pages, n_free, shared, outputs)
+    return _issue(_lib().fspad_page_fork, "fspad_page_fork", args, keep, tuple(outputs), prepare)
+
+
+def fspad_page_release_workspace_bytes(B: int, n_pages: int, table_width: int) -> int:
+    return int(_lib().fspad_page_release_workspace_bytes(int(B), int(n_pages), int(table_width)))
+
+
+def fspad_page_release(ended: torch.Tensor, kv_len: torch.Tensor, block_table: torch.Tensor, free_pages: torch.Tensor, n_free: torch.Tensor,
+                       shared: torch.Tensor, page_tokens: int, outputs=None, workspace: Optional[torch.Tensor] = None, stream=None,
+                       prepare: bool = False):
+    """Device int32 tensors: ended [B] (not 0: the sequence ends), the others as for fspad_page_fork; free_pages is written behind its first n_free
+    entries. Returns (kv_len_out [B], n_free_out [1], shared_out [n_pages]); `outputs` may bring them (kv_len, n_free and shared themselves: updated in
+    place). With prepare=True a PreparedCall."""
+    B, n_pages = kv_len.numel(), free_pages.numel()
+    _check_table(block_table, B)
+    if outputs is None:
+        outputs = _empty_i32(kv_len.device, (B,), (1,), (n_pages,))
+    kv_len_out, n_free_out, shared_out = outputs
+    _check_i32([("ended", ended, (B,)), ("kv_len", kv_len, (B,)), ("free_pages", free_pages, (n_pages,)), ("n_free", n_free, (1,)), ("shared", shared, (n_pages,)),
+                ("kv_len_out", kv_len_out, (B,)), ("n_free_out", n_free_out, (1,)), ("shared_out", shared_out, (n_pages,))])
+    if workspace is None:
+        workspace = torch.empty(max(16, fspad_page_release_workspace_bytes(B, n_pages, block_table.shape[1])), dtype=torch.uint8, device=kv_len.device)
+    args = (B, int(page_tokens), n_pages, block_table.shape[1], _row_stride(block_table), _dev_ptr(ended, "ended"), _dev_ptr(kv_len, "kv_len"),
+            _dev_ptr(block_table, "block_table"), _dev_ptr(free_pages, "free_pages"), _dev_ptr(n_free, "n_free"), _dev_ptr(shared, "shared"),
+            *(_dev_ptr(t, "outputs") for t in outputs), _dev_ptr(workspace, "workspace"), workspace.numel() * workspace.element_size(), _stream_ptr(stream))
+    _on_current_device(ended, kv_len, block_table, free_pages, n_free, shared, *outputs, workspace)
+    keep = (ended, kv_len, block_table, free_pages, n_free, shared, outputs, workspace)
+    return _issue(_lib().fspad_page_release, "fspad_page_release", args, keep, tuple(outputs), prepare)
+
+
+def fspad_page_compact_workspace_bytes(n_pages: int) -> int:
+    return int(_lib().fspad_page_compact_workspace_bytes(int(n_pages)))
+
+
+def fspad_page_compact(kv_len: torch.Tensor, block_table: torch.Tensor, free_pages: torch.Tensor, n_free: torch.Tensor, shared: torch.Tensor, page_tokens: int,
+                       outputs=None, workspace: Optional[torch.Tensor] = None, stream=None, prepare: bool = False):
+    """Device int32 tensors as for fspad_page_fork. Returns (copy_src [n_pages // 2], copy_dst [n_pages // 2], block_table_out [B,width], free_out [n_pages],
+    shared_out [n_pages]); `outputs` may bring them (block_table, free_pages and shared themselves as the last three: updated in place). With prepare=True
+    a PreparedCall. fspad_page_copy(copy_src, copy_dst, pages) of every pool belongs behind it."""
+    B, n_pages = kv_len.numel(), free_pages.numel()
+    _check_table(block_table, B)
+    if outputs is None:
+        outputs = _empty_i32(kv_len.device, (n_pages // 2,), (n_pages // 2,), tuple(block_table.shape), (n_pages,), (n_pages,))
+    copy_src, copy_dst, table_out, free_out, shared_out = outputs
+    _check_table(table_out, B, "block_table_out")
+    if table_out.shape != block_table.shape:
+        raise ValueError("block_table_out must have the shape of block_table")
+    _check_i32([("kv_len", kv_len, (B,)), ("free_pages", free_pages, (n_pages,)), ("n_free", n_free, (1,)), ("shared", shared, (n_pages,)),
+                ("copy_src", copy_src, (n_pages // 2,)), ("copy_dst", copy_dst, (n_pages // 2,)), ("free_out", free_out, (n_pages,)),
+                ("shared_out", shared_out, (n_pages,))])
+    if workspace is None:
+        workspace = torch.empty(max(16, fspad_page_compact_workspace_bytes(n_pages)), dtype=torch.uint8, device=kv_len.device)
+    args = (B, int(page_tokens), n_pages, block_table.shape[1], _row_stride(block_table), _row_stride(table_out), _dev_ptr(kv_len, "kv_len"),
+            _dev_ptr(block_table, "block_table"), _dev_ptr(free_pages, "free_pages"), _dev_ptr(n_free, "n_free"), _dev_ptr(shared, "shared"),
+            *(_dev_ptr(t, "outputs") for t in outputs), _dev_ptr(workspace, "workspace"), workspace.numel() * workspace.element_size(), _stream_ptr(stream))
+    _on_current_device(kv_len, block_table, free_pages, n_free, shared, *outputs, workspace)
+    keep = (kv_len, block_table, free_pages, n_free, shared, outputs, workspace)
+    return _issue(_lib().fspad_page_compact, "fspad_page_compact", args, keep, tuple(outputs), prepare)
+
+
+def fspad_page_copy(copy_src: torch.Tensor, copy_dst: torch.Tensor, pages: torch.Tensor, stream=None, prepare: bool = False):
+    """pages uint8 [n_pages, ...], the bytes of a page contiguous, pages any stride apart: page copy_dst[i] becomes what page copy_src[i] is, for all i where
+    both are pages. Device int32 tensors of one length. Returns pages; with prepare=True a PreparedCall."""
+    if pages.dtype != torch.uint8 or pages.dim() < 2 or (pages.shape[0] and not pages[0].is_contiguous()):
+        raise ValueError("pages must be a uint8 [n_pages, ...] device tensor, the bytes of a page contiguous")
+    n = copy_src.numel()
+    _check_i32([("copy_src", copy_src, (n,)), ("copy_dst", copy_dst, (n,))])
+    n_pages = pages.shape[0]
+    page_bytes = pages[0].numel() if n_pages else 0
+    args = (_dev_ptr(pages, "pages"), n_pages, pages.stride(0) if n_pages > 1 else page_bytes, page_bytes, n, _dev_ptr(copy_src, "copy_src"),
+            _dev_ptr(copy_dst, "copy_dst"), _stream_ptr(stream))
+    _on_current_device(copy_src, copy_dst, pages)
+    return _issue(_lib().fspad_page_copy, "fspad_page_copy", args, (copy_src, copy_dst, pages), pages, prepare)
 
 
 def fspad_draft_topk_workspace_bytes(rows: int, V: int, k: int) -> int:

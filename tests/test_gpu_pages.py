@@ -1,0 +1,185 @@
+"""GPU parity of forks, releases, compaction and copies of pages with the oracle, entry by entry."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2408_15562_amd as fspad
+from oracle import pages
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+def _dev(a):
+    return torch.from_numpy(np.ascontiguousarray(a, dtype=np.int32)).to(DEV)
+
+
+def _host(*tensors):
+    torch.cuda.synchronize()
+    return [t.cpu().numpy() for t in tensors]
+
+
+class State:
+    """Sequences in families of up to `share` that hold their first pages together, over a pool of more pages than they need; junk behind held
+    entries and behind the stack, some rows without tokens."""
+
+    def __init__(self, seed, B, P, n_pages, width, share=3, stride=None, bad=False):
+        rng = self.rng = np.random.default_rng(seed)
+        self.P, self.n_pages = P, n_pages
+        full = np.full((B, stride or width), 77, np.int64)
+        self.table = full[:, :width]
+        self.table[:] = rng.integers(-5, 2 * n_pages, (B, width))
+        self.lens, self.shared = np.zeros(B, np.int64), np.zeros(n_pages, np.int64)
+        order, at, b = rng.permutation(n_pages), 0, 0
+        while b < B:
+            n = int(rng.integers(1, share + 1))
+            if rng.random() < 0.3:                           # rows without tokens
+                b += n
+                continue
+            common = int(rng.integers(0, width))
+            if at + common + n * width > n_pages - 5:
+                break
+            for i in range(b, min(b + n, B)):
+                own = int(rng.integers(0, width - common + 1))
+                self.table[i, :common] = order[at:at + common]
+                self.table[i, common:common + own] = order[at + common + (i - b) * width:][:own]
+                self.lens[i] = (common + own) * P - (int(rng.integers(0, P)) if own else 0)
+            self.shared[order[at:at + common]] = min(n, B - b) - 1
+            at += common + n * width
+            b += n
+        held = {int(p) for i in range(B) for p in self.table[i, :-(-self.lens[i] // P)]}
+        rest = np.array([p for p in rng.permutation(n_pages) if p not in held])
+        self.free = np.concatenate([rest, rng.integers(-9, 2 * n_pages, n_pages - len(rest))])
+        self.n_free = np.array([len(rest)])
+        self.lens[self.lens == 0] = rng.integers(-3, 1, int((self.lens == 0).sum()))
+        if bad:                                              # entries that name no page
+            for i in range(0, B, 3):
+                if self.lens[i] > 0:
+                    self.table[i, int(rng.integers(0, -(-self.lens[i] // P)))] = [-1, n_pages, 2 ** 31 - 1, -2 ** 31][i % 4]
+        self.table_dev = torch.from_numpy(full.astype(np.int32)).to(DEV)[:, :width]
+
+    def args(self):
+        return (_dev(self.lens), self.table_dev, _dev(self.free), _dev(self.n_free), _dev(self.shared))
+
+    def host(self):
+        return self.lens, self.table, self.free, self.n_free, self.shared
+
+
+SIZES = [(1, 16, 8, 2), (5, 16, 60, 4), (40, 32, 900, 9), (300, 16, 9000, 20), (2048, 64, 40000, 13), (700, 16, 50000, 60)]
+
+
+@pytest.mark.parametrize("B,P,n_pages,width", SIZES)
+@pytest.mark.parametrize("place", ["apart", "in place", "bad entries"])
+def test_fork(B, P, n_pages, width, place):
+    s = State(B + n_pages, B, P, n_pages, width, stride=width + 3, bad=place == "bad entries")
+    rng = s.rng
+    F = max(1, min(2048, B // 2 + 3))
+    src, dst = rng.integers(0, B, F), rng.permutation(np.arange(B).repeat(2))[:F] if B > 2 else rng.integers(-1, B + 1, F)
+    empty = np.flatnonzero(s.lens <= 0)
+    if len(empty):
+        k = min(len(empty), F)
+        dst[rng.permutation(F)[:k]] = rng.permutation(empty)[:k]
+    odd = rng.permutation(F)[:F // 10]
+    src[odd[:len(odd) // 2]] = -1 - rng.integers(0, 5, len(odd) // 2)
+    dst[odd[len(odd) // 2:]] = B + rng.integers(0, 2 ** 20, len(odd) - len(odd) // 2)
+    n = np.array([rng.integers(-1, max(int(s.lens[x]), 0) + 2) if 0 <= x < B else 3 for x in src])
+    s.n_free[0] = min(s.n_free[0], max(1, F // 3))           # too few for all of them
+    for n_tokens in (None, n):
+        lens, table, free, n_free, shared = s.args()
+        before = table.clone()
+        want = pages.fork(src, dst, *s.host(), P, n_tokens=n_tokens)
+        outputs = None
+        if place == "in place":
+            outputs = (*(torch.empty(F, dtype=torch.int32, device=DEV) for _ in range(2)), lens, n_free, shared, torch.empty(F, dtype=torch.int32, device=DEV))
+        got = fspad.fspad_page_fork(_dev(src), _dev(dst), lens, table, free, n_free, shared, P, n_tokens=None if n_tokens is None else _dev(n_tokens), outputs=outputs)
+        for name, g, w in zip(("copy_src", "copy_dst", "kv_len", "n_free", "shared", "granted", "table"), _host(*got, table), want):
+            assert np.array_equal(g, w), name
+        assert np.array_equal(_host(free)[0], s.free)
+        if B > 2:
+            assert want[5].any()
+        table.copy_(before)
+
+
+@pytest.mark.parametrize("B,P,n_pages,width", SIZES)
+@pytest.mark.parametrize("place", ["apart", "in place", "bad entries"])
+@pytest.mark.parametrize("part", [0.0, 0.4, 1.0])
+def test_release(B, P, n_pages, width, place, part):
+    s = State(B + width, B, P, n_pages, width, stride=width + 2, bad=place == "bad entries")
+    ended = (s.rng.random(B) < part) * s.rng.integers(1, 9, B)
+    if part < 1:
+        s.shared[s.rng.integers(0, n_pages, 3)] -= 1         # (below zero in places: taken as zero)
+    want = pages.release(ended, *s.host(), P)
+    lens, table, free, n_free, shared = s.args()
+    before = table.clone()
+    size = fspad.fspad_page_release_workspace_bytes(B, n_pages, width)
+    ws = torch.full((size + 64,), 0xA5, dtype=torch.uint8, device=DEV)
+    got = fspad.fspad_page_release(_dev(ended), lens, table, free, n_free, shared, P, outputs=(lens, n_free, shared) if place == "in place" else None, workspace=ws[:size] if size else None)
+    for name, g, w in zip(("kv_len", "n_free", "shared", "free"), _host(*got, free), want):
+        assert np.array_equal(g, w), name
+    assert torch.equal(table, before) and bool((ws[size:] == 0xA5).all())
+
+
+@pytest.mark.parametrize("B,P,n_pages,width", SIZES + [(3, 16, 1, 2), (2, 16, 31, 3), (2, 16, 32, 3), (2, 16, 33, 3), (9, 16, 1 << 20, 4)])
+@pytest.mark.parametrize("place", ["apart", "in place", "bad entries"])
+def test_compact(B, P, n_pages, width, place):
+    s = State(B * width, B, P, n_pages, width, stride=width + 1, bad=place == "bad entries")
+    want = pages.compact(*s.host(), P)
+    lens, table, free, n_free, shared = s.args()
+    size = fspad.fspad_page_compact_workspace_bytes(n_pages)
+    ws = torch.full((size + 64,), 0xA5, dtype=torch.uint8, device=DEV)
+    outputs = None
+    if place == "in place":
+        outputs = (*(torch.empty(n_pages // 2, dtype=torch.int32, device=DEV) for _ in range(2)), table, free, shared)
+    got = fspad.fspad_page_compact(lens, table, free, n_free, shared, P, outputs=outputs, workspace=ws[:size])
+    for name, g, w in zip(("copy_src", "copy_dst", "table", "free", "shared"), _host(*got), want):
+        assert np.array_equal(g, w), name
+    assert bool((ws[size:] == 0xA5).all())
+    base = table._base if table._base is not None else table
+    assert bool((base[:, width:] == 77).all())
+
+
+@pytest.mark.parametrize("n_free", [0, 1, 16, 31, 32, 33])
+def test_compact_of_full_and_empty_pools(n_free):
+    n_pages, P = 33, 16
+    rng = np.random.default_rng(n_free)
+    order = rng.permutation(n_pages)
+    held = order[n_free:]
+    table, lens = np.full((1, max(1, len(held))), -1), np.array([len(held) * P])
+    table[0, :len(held)] = held
+    free = np.concatenate([order[:n_free], np.full(n_pages - n_free, -1)])
+    shared = rng.integers(0, 5, n_pages)
+    want = pages.compact(lens, table, free, [n_free], shared, P)
+    got = fspad.fspad_page_compact(_dev(lens), _dev(table), _dev(free), _dev([n_free]), _dev(shared), P)
+    for g, w in zip(_host(*got), want):
+        assert np.array_equal(g, w)
+
+
+@pytest.mark.parametrize("shape", [(9, 16), (40, 2, 1072), (5, 8, 16400), (300, 17408 * 3)])
+def test_copy(shape):
+    rng = np.random.default_rng(shape[0])
+    pool = torch.randint(0, 256, (shape[0], 2, *shape[1:]), dtype=torch.uint8, device=DEV)
+    order = rng.permutation(shape[0])
+    n = shape[0] // 2
+    src, dst = np.concatenate([order[:n], [-1, order[0], shape[0], 0, 2 ** 31 - 1]]), np.concatenate([order[n:2 * n], [order[-1], -1, order[-1], -2 ** 31, 1]])
+    want = pages.copy(pool[:, 1].cpu().numpy(), src, dst)
+    other = pool[:, 0].clone()
+    fspad.fspad_page_copy(_dev(src), _dev(dst), pool[:, 1])      # one layer of two
+    torch.cuda.synchronize()
+    assert np.array_equal(pool[:, 1].cpu().numpy(), want) and torch.equal(pool[:, 0], other)
+    both = pool.cpu().numpy()
+    fspad.fspad_page_copy(_dev(src), _dev(dst), pool)            # both
+    torch.cuda.synchronize()
+    assert np.array_equal(pool.cpu().numpy(), pages.copy(both, src, dst))
+    fspad.fspad_page_copy(_dev([]), _dev([]), pool)
+
+
+def test_copy_past_32_bits_of_bytes():
+    per = 8 * 65552
+    n_pages = (1 << 32) // per + 9
+    pool = torch.zeros((n_pages, per), dtype=torch.uint8, device=DEV)
+    pool[n_pages - 1] = torch.randint(1, 256, (per,), dtype=torch.uint8, device=DEV)
+    pool[1] = 5
+    fspad.fspad_page_copy(_dev([n_pages - 1, 1]), _dev([3, n_pages - 2]), pool)
+    torch.cuda.synchronize()
+    assert torch.equal(pool[3], pool[n_pages - 1]) and bool((pool[n_pages - 2] == 5).all())
+    assert bool((pool[[0, 2, 4, n_pages - 3]] == 0).all())

@@ -578,7 +578,7 @@ fspad_status fspad_tree_attn_paged_byte(const fspad_paged_desc* desc,
  * any may be shared end by fspad_page_release, not by n_new < 0. Only full pages are ever shared, so that growth writes to pages of a
  * sequence's own. The calls are about block tables: they serve the 4-bit and the 8-bit cache alike, all layers at once.
  *
- *   B           rows of the block table, 1..2048;  page_tokens 16, 32, 64, 128 or 256;  n_pages 1..2^20 (n_pages and table_width times page_tokens <= 2^31 - 1)
+ *   B           rows of the block table, 1..2048;  page_tokens 16, 32, 64, 128 or 256;  n_pages 1..2^19 (n_pages and table_width times page_tokens <= 2^31 - 1)
  *   block_table dev [B] rows of table_width i32, table_stride entries apart (B * table_width <= 2^30)
  *   kv_len      dev [B] i32 (negative lengths count as 0); sequence b holds the first ceil(kv_len[b] / P) entries of its row
  *   free_pages  dev [n_pages] i32, n_free dev [1] i32 (taken as 0..n_pages): the stack of fspad_page_map. It names no page twice and none that is held
@@ -629,16 +629,13 @@ fspad_status fspad_page_release(int32_t B, int32_t page_tokens, int32_t n_pages,
  *   copy_src, copy_dst   dev [n_pages / 2] i32 out (may be NULL if n_pages is 1)
  *   block_table_out      dev [B] rows of table_width i32, out_stride entries apart: may be block_table (with its stride); else entries that are not held are copied
  *   free_out, shared_out dev [n_pages] i32 out: may be free_pages and shared
- *   workspace   dev, 16-byte aligned, >= fspad_page_compact_workspace_bytes(n_pages); contents ignored on entry, undefined on exit; two calls
- *               that may overlap in time need different ones
+ * No workspace.
  */
-size_t fspad_page_compact_workspace_bytes(int32_t n_pages);
-
 fspad_status fspad_page_compact(int32_t B, int32_t page_tokens, int32_t n_pages, int32_t table_width, int64_t table_stride, int64_t out_stride,
                                 const int32_t* kv_len, const int32_t* block_table, const int32_t* free_pages,
                                 const int32_t* n_free, const int32_t* shared, int32_t* copy_src, int32_t* copy_dst,
                                 int32_t* block_table_out, int32_t* free_out, int32_t* shared_out,
-                                void* workspace, size_t workspace_bytes, void* hip_stream);
+                                void* hip_stream);
 
 /*
  * Copies: page copy_dst[i] of a pool becomes what page copy_src[i] is, for i < n_copies where both lie in [0,n_pages) (other pairs are passed over). No

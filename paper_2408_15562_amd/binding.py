@@ -35,7 +35,7 @@ EXPORTS = ("fspad_tree_attn_workspace_bytes", "fspad_tree_attn",
            "fspad_tree_attn_paged_workspace_bytes", "fspad_tree_attn_paged",
            "fspad_kv_page_bytes_byte", "fspad_kv_store_paged_byte_workspace_bytes", "fspad_kv_store_paged_byte", "fspad_kv_load_paged_byte",
            "fspad_tree_attn_paged_byte_workspace_bytes", "fspad_tree_attn_paged_byte",
-           "fspad_page_fork", "fspad_page_release_workspace_bytes", "fspad_page_release", "fspad_page_compact_workspace_bytes", "fspad_page_compact",
+           "fspad_page_fork", "fspad_page_release_workspace_bytes", "fspad_page_release", "fspad_page_compact",
            "fspad_page_copy",
            "fspad_draft_topk_workspace_bytes", "fspad_draft_topk", "fspad_tree_build", "fspad_tree_build_mask",
            "fspad_tree_validate", "fspad_status_string")
@@ -160,10 +160,8 @@ def _lib():
         lib.fspad_page_release_workspace_bytes.argtypes = [i32, i32, i32]
         lib.fspad_page_release.restype = ctypes.c_int
         lib.fspad_page_release.argtypes = [i32, i32, i32, i32, i64] + [vp] * 9 + [vp, sz, vp]
-        lib.fspad_page_compact_workspace_bytes.restype = sz
-        lib.fspad_page_compact_workspace_bytes.argtypes = [i32]
         lib.fspad_page_compact.restype = ctypes.c_int
-        lib.fspad_page_compact.argtypes = [i32, i32, i32, i32, i64, i64] + [vp] * 10 + [vp, sz, vp]
+        lib.fspad_page_compact.argtypes = [i32, i32, i32, i32, i64, i64] + [vp] * 11
         lib.fspad_page_copy.restype = ctypes.c_int
         lib.fspad_page_copy.argtypes = [vp, i32, i64, i64, i32, vp, vp, vp]
         lib.fspad_draft_topk_workspace_bytes.restype = sz
@@ -992,12 +990,8 @@ def fspad_page_release(ended: torch.Tensor, kv_len: torch.Tensor, block_table: t
     return _issue(_lib().fspad_page_release, "fspad_page_release", args, keep, tuple(outputs), prepare)
 
 
-def fspad_page_compact_workspace_bytes(n_pages: int) -> int:
-    return int(_lib().fspad_page_compact_workspace_bytes(int(n_pages)))
-
-
 def fspad_page_compact(kv_len: torch.Tensor, block_table: torch.Tensor, free_pages: torch.Tensor, n_free: torch.Tensor, shared: torch.Tensor, page_tokens: int,
-                       outputs=None, workspace: Optional[torch.Tensor] = None, stream=None, prepare: bool = False):
+                       outputs=None, stream=None, prepare: bool = False):
     """Device int32 tensors as for fspad_page_fork. Returns (copy_src [n_pages // 2], copy_dst [n_pages // 2], block_table_out [B,width], free_out [n_pages],
     shared_out [n_pages]); `outputs` may bring them (block_table, free_pages and shared themselves as the last three: updated in place). With prepare=True
     a PreparedCall. fspad_page_copy(copy_src, copy_dst, pages) of every pool belongs behind it."""
@@ -1012,13 +1006,11 @@ def fspad_page_compact(kv_len: torch.Tensor, block_table: torch.Tensor, free_pag
     _check_i32([("kv_len", kv_len, (B,)), ("free_pages", free_pages, (n_pages,)), ("n_free", n_free, (1,)), ("shared", shared, (n_pages,)),
                 ("copy_src", copy_src, (n_pages // 2,)), ("copy_dst", copy_dst, (n_pages // 2,)), ("free_out", free_out, (n_pages,)),
                 ("shared_out", shared_out, (n_pages,))])
-    if workspace is None:
-        workspace = torch.empty(max(16, fspad_page_compact_workspace_bytes(n_pages)), dtype=torch.uint8, device=kv_len.device)
     args = (B, int(page_tokens), n_pages, block_table.shape[1], _row_stride(block_table), _row_stride(table_out), _dev_ptr(kv_len, "kv_len"),
             _dev_ptr(block_table, "block_table"), _dev_ptr(free_pages, "free_pages"), _dev_ptr(n_free, "n_free"), _dev_ptr(shared, "shared"),
-            *(_dev_ptr(t, "outputs") for t in outputs), _dev_ptr(workspace, "workspace"), workspace.numel() * workspace.element_size(), _stream_ptr(stream))
-    _on_current_device(kv_len, block_table, free_pages, n_free, shared, *outputs, workspace)
-    keep = (kv_len, block_table, free_pages, n_free, shared, outputs, workspace)
+            *(_dev_ptr(t, "outputs") for t in outputs), _stream_ptr(stream))
+    _on_current_device(kv_len, block_table, free_pages, n_free, shared, *outputs)
+    keep = (kv_len, block_table, free_pages, n_free, shared, outputs)
     return _issue(_lib().fspad_page_compact, "fspad_page_compact", args, keep, tuple(outputs), prepare)
 
 

@@ -65,7 +65,7 @@ class State:
         return self.lens, self.table, self.free, self.n_free, self.shared
 
 
-SIZES = [(1, 16, 8, 2), (5, 16, 60, 4), (40, 32, 900, 9), (300, 16, 9000, 20), (2048, 64, 40000, 13), (700, 16, 50000, 60)]
+SIZES = [(1, 16, 8, 2), (5, 16, 60, 4), (40, 32, 900, 9), (300, 16, 9000, 20), (2048, 64, 40000, 13), (700, 16, 50000, 60), (64, 16, 16384, 200), (33, 16, 16385, 200)]
 
 
 @pytest.mark.parametrize("B,P,n_pages,width", SIZES)
@@ -119,21 +119,18 @@ def test_release(B, P, n_pages, width, place, part):
     assert torch.equal(table, before) and bool((ws[size:] == 0xA5).all())
 
 
-@pytest.mark.parametrize("B,P,n_pages,width", SIZES + [(3, 16, 1, 2), (2, 16, 31, 3), (2, 16, 32, 3), (2, 16, 33, 3), (9, 16, 1 << 20, 4)])
+@pytest.mark.parametrize("B,P,n_pages,width", SIZES + [(3, 16, 1, 2), (2, 16, 31, 3), (2, 16, 32, 3), (2, 16, 33, 3), (9, 16, 1 << 19, 4), (4, 16, 16384, 3000)])
 @pytest.mark.parametrize("place", ["apart", "in place", "bad entries"])
 def test_compact(B, P, n_pages, width, place):
     s = State(B * width, B, P, n_pages, width, stride=width + 1, bad=place == "bad entries")
     want = pages.compact(*s.host(), P)
     lens, table, free, n_free, shared = s.args()
-    size = fspad.fspad_page_compact_workspace_bytes(n_pages)
-    ws = torch.full((size + 64,), 0xA5, dtype=torch.uint8, device=DEV)
     outputs = None
     if place == "in place":
         outputs = (*(torch.empty(n_pages // 2, dtype=torch.int32, device=DEV) for _ in range(2)), table, free, shared)
-    got = fspad.fspad_page_compact(lens, table, free, n_free, shared, P, outputs=outputs, workspace=ws[:size])
+    got = fspad.fspad_page_compact(lens, table, free, n_free, shared, P, outputs=outputs)
     for name, g, w in zip(("copy_src", "copy_dst", "table", "free", "shared"), _host(*got), want):
         assert np.array_equal(g, w), name
-    assert bool((ws[size:] == 0xA5).all())
     base = table._base if table._base is not None else table
     assert bool((base[:, width:] == 77).all())
 

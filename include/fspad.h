@@ -544,7 +544,7 @@ size_t fspad_kv_page_bytes_byte(int32_t n_kv_heads, int32_t head_dim, int32_t pa
  *             call (what the block holds of it then is not specified)
  *   rows      0..1048560; 0 does nothing (no pointer is looked at)
  *   pages     dev, 16-byte aligned. Tokens of other blocks stay as they are; no other call may use a block that this one stores to meanwhile
- *   workspace dev, 16-byte aligned, >= fspad_kv_store_paged_byte_workspace_bytes(desc, rows): 0 up to 1024 rows (may be NULL then), 4 bytes a
+ *   workspace dev, 16-byte aligned, >= fspad_kv_store_paged_byte_workspace_bytes(desc, rows): 0 up to 16384 rows (may be NULL then), 4 bytes a
  *             slot of the pool for more; contents ignored on entry, undefined on exit; two calls that may overlap in time need different ones
  * Reads n_kv_heads, head_dim, io_dtype, page_tokens, n_pages and page_stride of the descriptor, as fspad_kv_load_paged_byte does.
  */

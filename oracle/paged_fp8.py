@@ -68,9 +68,11 @@ class Fp8Pages:
     def store(self, which: str, x, slots):
         """Rows x [rows, Hkv, D] into slots, block by block."""
         slots = np.asarray(slots, np.int64)
-        live = [r for r in range(len(slots)) if 0 <= slots[r] < len(self.raw) * self.P]
-        for block in sorted({int(slots[r]) // BLOCK for r in live}):
-            rows = [r for r in live if slots[r] // BLOCK == block]
+        blocks = {}
+        for r in range(len(slots)):
+            if 0 <= slots[r] < len(self.raw) * self.P:
+                blocks.setdefault(int(slots[r]) // BLOCK, []).append(r)
+        for block, rows in blocks.items():
             begun = any(slots[r] % BLOCK == 0 for r in rows)
             first = block * BLOCK
             for head in range(self.raw.shape[1]):

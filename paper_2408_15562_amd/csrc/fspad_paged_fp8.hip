@@ -6,6 +6,7 @@
 
 #include "fspad.h"
 #include "paged_layout.h"
+#include "wave_scan.h"
 
 namespace {
 
@@ -29,12 +30,8 @@ struct RowsParams {
   int32_t rows, n_slots, page_shift;
 };
 
-// Where channel c of token t of a block lies among the block's codes.
-template <int D>
+// Where channel c of token t of a block lies among the block's codes of K.
 __device__ __forceinline__ int k_code_at(int t, int c) { return ((c >> 4) * kBlock + t) * 16 + (c & 15); }
-template <int D>
-__device__ __forceinline__ int v_code_at(int t, int c) { return ((c % (D / 32) * 2 + (t >> 4)) * 32 + c / (D / 32)) * 16 + (t & 15); }
-
 template <int D>
 __device__ __forceinline__ char* head_of(const RowsParams& p, int slot, int head) {
   return p.pages + (int64_t)(slot >> p.page_shift) * p.page_stride + (int64_t)head * page_head_bytes_fp8(D, 1 << p.page_shift);
@@ -51,15 +48,15 @@ __device__ __forceinline__ float as_scale(int s) { return __builtin_bit_cast(flo
 
 __device__ __forceinline__ unsigned finite_or_zero(unsigned magnitude) { return magnitude < 0x7f80u ? magnitude : 0u; }
 __device__ __forceinline__ unsigned at_most_top(unsigned bits) { return (bits & 0x7fffu) < 0x7f80u ? (bits & 0x8000u) | min(bits & 0x7fffu, kTopBits) : bits; }
-__device__ __forceinline__ unsigned has_wild(unsigned w) { return ((w & 0x7f807f80u) + 0x00800080u) & 0x80008000u; }
 
-// Four channels to codes: rounded to nearest, ties to even. NaN and infinity become NaN (all bits below the sign).
+// Four channels to codes: rounded to nearest, ties to even. WILD: some are NaN or infinite, which become NaN (all bits below the sign).
+template <bool WILD>
 __device__ __forceinline__ unsigned encode4(unsigned low, unsigned high, float scale) {
   s16x2 c = {0, 0};
   c = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(c, __builtin_bit_cast(bf16x2, low), scale, false);
   c = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(c, __builtin_bit_cast(bf16x2, high), scale, true);
   unsigned codes = __builtin_bit_cast(unsigned, c);
-  if (__builtin_expect((has_wild(low) | has_wild(high)) != 0, 0)) {
+  if constexpr (WILD) {
     codes |= (low & 0x7f80u) == 0x7f80u ? 0x7fu : 0u;
     codes |= (low & 0x7f800000u) == 0x7f800000u ? 0x7f00u : 0u;
     codes |= (high & 0x7f80u) == 0x7f80u ? 0x7f0000u : 0u;
@@ -74,16 +71,22 @@ __device__ __forceinline__ u32x2 decode4(unsigned codes, float scale) {
 // Codes under one scale, rounded again under a larger one.
 __device__ __forceinline__ unsigned again4(unsigned codes, float had, float scale) {
   const u32x2 x = decode4(codes, had);
-  return encode4(x[0], x[1], scale);
+  return encode4<true>(x[0], x[1], scale);
 }
 
 // ---------------------------------------------------------------------------------------------
-// Store. A block's scale is that of all its tokens, so one workgroup has all of a call's rows of a block (and one head): it looks for
+// Store. A block's scale is that of all its tokens, so whoever stores to a block (of a head) has all of a call's rows of it: looks for
 // them, forms the largest magnitude, rounds, and where the scale of a block that holds tokens grows rounds those again. The rows of a block
-// may stand anywhere in the call. Which they are is found by looking through all of a call's slots where those are few, else in a
-// list by slot that a launch before this one writes; the row that has the block's lowest place leads, and its workgroup does the block.
-constexpr int kScanRows = 1024;   // at most, without the list
-constexpr int kChunk = 16;        // rows that a workgroup looks after, with it
+// may stand anywhere in the call. A workgroup looks after some neighbouring rows, block by block. Are all of a block's tokens in neighbouring rows (a prompt's are), it sees that
+// from the slots of these and some rows around them. Else it goes through all of the call's slots, or, of many rows, through
+// a list by slot that a launch before this one writes. The block is that workgroup's whose rows have the block's lowest token.
+//
+// Groups of 256 threads have a head each. Every thread has a piece of K and of V the channels of four neighbouring tokens that make four neighbouring bytes of
+// D/32 places: what it rounds it stores, whole lines a wavefront.
+constexpr int kScanRows = 16384;   // at most, without the list
+constexpr int kMostChunk = 32;     // rows that a workgroup looks after
+constexpr int kWindow = kMostChunk + 2 * (kBlock - 1);   // and sees
+constexpr int kEnoughWorkgroups = 1024, kHeadsAtOnce = 2, kMostHeads = 4;
 
 __global__ __launch_bounds__(kThreads) void kv_rows_of_slots_kernel(const RowsParams p) {
   const int row = blockIdx.x * kThreads + threadIdx.x;
@@ -92,152 +95,275 @@ __global__ __launch_bounds__(kThreads) void kv_rows_of_slots_kernel(const RowsPa
   if ((unsigned)slot < (unsigned)p.n_slots) p.row_of[slot] = row;
 }
 
+template <int HEADS>
 struct StoreShared {
-  int member[kChunk][kBlock];   // row of each token of a row's block, -1: none
-  unsigned there[kChunk];       // bit t: token t has one
-  unsigned top[2][kThreads / 64];
-  alignas(16) unsigned char codes[2][kBlock * 128];
+  int slot[kWindow];        // of rows row0 - 31 .., -1 outside the call or the pool
+  int member[kBlock];       // the row of each token of the block at hand
+  unsigned top[2][HEADS][2][kThreads / 64];
 };
 
-// One block of one head. member: its rows; there: which tokens have one.
-template <int D>
-__device__ __forceinline__ void store_block(const RowsParams& p, StoreShared& sh, const int* member, unsigned there, int slot0, int head) {
-  constexpr int LPR = D / 8, TOKENS = kThreads / LPR, PASSES = kBlock / TOKENS;   // lanes of a row; rows at a time
-  const int P = 1 << p.page_shift, tid = threadIdx.x, part = tid % LPR;
-  char* base = head_of<D>(p, slot0, head);
-  const int nth = (slot0 & (P - 1)) / kBlock;
-  char* codes[2] = {base + nth * (kBlock * D), base + P * D + nth * (kBlock * D)};
-  unsigned char* scales[2] = {(unsigned char*)base + 2 * P * D + nth, (unsigned char*)base + 2 * P * D + kFp8VScales + nth};
-  u32x4 x[PASSES][2];
-  unsigned top[2] = {0, 0};
+typedef __attribute__((ext_vector_type(2))) unsigned short u16x2;
+
+// Largest magnitude (bits) of some words of two values each. Magnitudes of bf16 compare as integers, infinity and NaN (from 0x7f80 on) above the rest.
+template <int N>
+__device__ __forceinline__ unsigned top_of(const unsigned (&w)[N]) {
+  u16x2 m = {0, 0};
 #pragma unroll
-  for (int i = 0; i < PASSES; ++i) {
-    const int t = i * TOKENS + tid / LPR, row = member[t];
-    x[i][0] = x[i][1] = u32x4{0u, 0u, 0u, 0u};
-    if ((there >> t) & 1u) {
-      const int64_t at = row * p.row_stride + head * p.head_stride + part * 16;
-      x[i][0] = *reinterpret_cast<const u32x4*>(p.k + at);
-      x[i][1] = *reinterpret_cast<const u32x4*>(p.v + at);
-    }
-  }
-  const bool begun = there & 1u;
-  int had[2] = {0, 0};
-  if (!begun) {
-    had[0] = *scales[0];
-    had[1] = *scales[1];
-  }
+  for (int i = 0; i < N; ++i) m = __builtin_elementwise_max(m, __builtin_bit_cast(u16x2, w[i] & 0x7fff7fffu));
+  return max((unsigned)m[0], (unsigned)m[1]);
+}
+template <int N>
+__device__ __forceinline__ unsigned finite_top_of(const unsigned (&w)[N]) {
+  unsigned top = 0;
 #pragma unroll
-  for (int i = 0; i < PASSES; ++i)
-#pragma unroll
-    for (int kv = 0; kv < 2; ++kv)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) top[kv] = max(top[kv], max(finite_or_zero(x[i][kv][j] & 0x7fffu), finite_or_zero((x[i][kv][j] >> 16) & 0x7fffu)));
-#pragma unroll
-  for (int kv = 0; kv < 2; ++kv) {
-#pragma unroll
-    for (int off = 32; off > 0; off >>= 1) top[kv] = max(top[kv], (unsigned)__shfl_xor((int)top[kv], off));
-    if ((tid & 63) == 0) sh.top[kv][tid >> 6] = top[kv];
-  }
-  __syncthreads();
-  int s[2];
-#pragma unroll
-  for (int kv = 0; kv < 2; ++kv) {
-    unsigned all = 0;
-#pragma unroll
-    for (int w = 0; w < kThreads / 64; ++w) all = max(all, sh.top[kv][w]);
-    s[kv] = max(scale_for(all), had[kv]);
-    if (__builtin_expect(all > kTopBits, 0)) {
-#pragma unroll
-      for (int i = 0; i < PASSES; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) x[i][kv][j] = at_most_top(x[i][kv][j] & 0xffffu) | at_most_top(x[i][kv][j] >> 16) << 16;
-    }
-  }
-  // codes of the new tokens, in the block's order
-#pragma unroll
-  for (int i = 0; i < PASSES; ++i) {
-    const int t = i * TOKENS + tid / LPR;
-    const u32x2 kc = {encode4(x[i][0][0], x[i][0][1], as_scale(s[0])), encode4(x[i][0][2], x[i][0][3], as_scale(s[0]))};
-    *reinterpret_cast<u32x2*>(&sh.codes[0][k_code_at<D>(t, part * 8)]) = kc;
-    const u32x2 vc = {encode4(x[i][1][0], x[i][1][1], as_scale(s[1])), encode4(x[i][1][2], x[i][1][3], as_scale(s[1]))};
-#pragma unroll
-    for (int j = 0; j < 8; ++j) sh.codes[1][v_code_at<D>(t, part * 8 + j)] = (unsigned char)(vc[j >> 2] >> (8 * (j & 3)));
-  }
-  __syncthreads();
-  // 16 bytes at a time: of K one token's, of V sixteen tokens' of one channel
-  for (int i = tid; i < kBlock * D / 16; i += kThreads) {
-    const int at = i * 16, t = i % kBlock, group = (i >> 5) & 1;
-    u32x4* const k_to = reinterpret_cast<u32x4*>(codes[0] + at);
-    if ((there >> t) & 1u) {
-      *k_to = *reinterpret_cast<const u32x4*>(&sh.codes[0][at]);
-    } else if (!begun && s[0] > had[0]) {
-      u32x4 c = *k_to;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) c[j] = again4(c[j], as_scale(had[0]), as_scale(s[0]));
-      *k_to = c;
-    }
-    const unsigned mine = (there >> (16 * group)) & 0xffffu;
-    const bool grown = !begun && s[1] > had[1];
-    if (mine || grown) {
-      u32x4* const v_to = reinterpret_cast<u32x4*>(codes[1] + at);
-      u32x4 c = *reinterpret_cast<const u32x4*>(&sh.codes[1][at]);
-      if (mine != 0xffffu) {
-        const u32x4 was = *v_to;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const unsigned bytes = (((mine >> (4 * j) & 15u) * 0x00204081u) & 0x01010101u) * 0xffu;
-          c[j] = (c[j] & bytes) | ((grown ? again4(was[j], as_scale(had[1]), as_scale(s[1])) : was[j]) & ~bytes);
-        }
-      }
-      *v_to = c;
-    }
-  }
-  if (tid < 2 && (begun || s[tid] > had[tid])) *scales[tid] = (unsigned char)s[tid];
+  for (int i = 0; i < N; ++i) top = max(top, max(finite_or_zero(w[i] & 0x7fffu), finite_or_zero((w[i] >> 16) & 0x7fffu)));
+  return top;
 }
 
-template <int D, bool SCAN>
-__global__ __launch_bounds__(kThreads) void kv_store_paged_fp8_kernel(const RowsParams p) {
-  __shared__ StoreShared sh;
-  const int head = blockIdx.x, tid = threadIdx.x;
-  if constexpr (SCAN) {   // a workgroup looks after one row
-    const int row = blockIdx.y, slot = p.slots[row];
-    if ((unsigned)slot >= (unsigned)p.n_slots) return;
-    if (tid < kBlock) sh.member[0][tid] = INT_MAX;
-    __syncthreads();
-    for (int i = tid; i < p.rows; i += kThreads) {
-      const unsigned off = (unsigned)p.slots[i] - (unsigned)(slot & -kBlock);
-      if (off < (unsigned)kBlock) atomicMin(&sh.member[0][off], i);   // (of a slot that two rows have the first one has it)
-    }
-    __syncthreads();
-    const unsigned there = (unsigned)__ballot(sh.member[0][tid & (kBlock - 1)] != INT_MAX);
-    if (sh.member[0][__builtin_ctz(there)] != row) return;
-    store_block<D>(p, sh, sh.member[0], there, slot & -kBlock, head);
-  } else {
-    // half a wavefront a row
-    const int row0 = blockIdx.y * kChunk, t = tid & (kBlock - 1);
-    for (int r = tid / kBlock; r < kChunk; r += kThreads / kBlock) {
-      const int row = row0 + r, slot = row < p.rows ? p.slots[row] : -1;
-      const bool valid = (unsigned)slot < (unsigned)p.n_slots;
-      int other = -1;
-      if (valid) {
-        const int place = (slot & -kBlock) + t;
-        const int x = p.row_of[place];
-        if ((unsigned)x < (unsigned)p.rows && p.slots[x] == place) other = x;
+__device__ __forceinline__ unsigned bytes_of(unsigned bits) { return (((bits & 15u) * 0x00204081u) & 0x01010101u) * 0xffu; }
+
+// A thread's part of a block of one head: of K, 8 channels of two tokens, which it makes 16 of one with its neighbour (loads of 16 channels a lane, in two
+// halves, would ask for every line twice); of V, the E channels of four tokens.
+// ALL: every token of the block has a row.
+template <int D, bool ALL>
+struct StorePart {
+  static constexpr int LANES = D / 8, E = D / 32, VW = E / 2;   // lanes of a token of K, words of one of V
+  static constexpr bool SOME = kBlock * LANES < 2 * kThreads;   // (K has no part for some threads)
+
+  // what is the same for all heads
+  struct Place {
+    const char *k[2], *v[4];
+    int k_at, v_at;                 // bytes from the block's codes on
+    unsigned has_k, own_k, has_v;   // bit i: token i of two (of four) is there; whether the one is that the thread stores
+  };
+  __device__ static __forceinline__ Place place(const RowsParams& p, const int* member, unsigned there) {
+    const int tid = threadIdx.x % kThreads, pair = tid / LANES, lane = tid % LANES;
+    const int first = 16 * ((tid >> 6) & 1) + 4 * (tid & 3), row = 16 * (tid >> 7) + ((tid >> 2) & 15);
+    const bool has_part = !SOME || 2 * pair < kBlock;
+    Place x;
+    x.has_k = !has_part ? 0u : ALL ? 3u : (there >> (2 * pair)) & 3u;
+    x.own_k = (x.has_k >> (lane & 1)) & 1u;
+    x.has_v = ALL ? 15u : (there >> first) & 15u;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) x.k[i] = p.k + ((x.has_k >> i) & 1u ? member[2 * pair + i] : 0) * p.row_stride + lane * 16;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x.v[i] = p.v + ((x.has_v >> i) & 1u ? member[first + i] : 0) * p.row_stride + row * (2 * E);
+    x.k_at = has_part ? ((lane >> 1) * kBlock + 2 * pair + (lane & 1)) * 16 : -1;
+    x.v_at = ((first >> 4) * 32 + row) * 16 + (first & 15);
+    return x;
+  }
+
+  unsigned k[8], v[4 * VW];   // (k: four words a token)
+  int had[2];
+
+  // head: bytes from a row's first head on
+  __device__ __forceinline__ void load(const Place& x, int64_t head, bool begun, const unsigned char* scales) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) k[i] = 0;
+#pragma unroll
+    for (int i = 0; i < 4 * VW; ++i) v[i] = 0;
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      if ((ALL && !SOME) || ((x.has_k >> i) & 1u)) {
+        const u32x4 w = *reinterpret_cast<const u32x4*>(x.k[i] + head);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) k[4 * i + j] = w[j];
       }
-      unsigned there = (unsigned)(__ballot(other >= 0) >> (tid & kBlock));
-      const int first = __shfl(other, (tid & kBlock) + (there ? __builtin_ctz(there) : 0));
-      if (!valid || first != row) there = 0;   // (nothing to do, or another row leads)
-      sh.member[r][t] = other;
-      if (t == 0) sh.there[r] = there;
-    }
-    __syncthreads();
-    for (int r = 0; r < kChunk; ++r) {
-      const unsigned there = sh.there[r];
-      if (there == 0) continue;
-      store_block<D>(p, sh, sh.member[r], there, p.slots[row0 + r] & -kBlock, head);
-      __syncthreads();   // (the codes' buffer is used again)
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (ALL || ((x.has_v >> i) & 1u)) {
+        if constexpr (E == 4) {
+          const u32x2 w = *reinterpret_cast<const u32x2*>(x.v[i] + head);
+          v[VW * i] = w[0];
+          v[VW * i + VW - 1] = w[1];
+        } else {
+          v[i] = *reinterpret_cast<const unsigned*>(x.v[i] + head);
+        }
+      }
+    had[0] = had[1] = 0;
+    if (!ALL && !begun) {
+      had[0] = scales[0];
+      had[1] = scales[kFp8VScales];
     }
   }
+
+  template <bool WILD>
+  __device__ __forceinline__ void encode(u32x4& kc, unsigned (&vc)[E], float k_scale, float v_scale) const {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) kc[i] = encode4<WILD>(k[2 * i], k[2 * i + 1], k_scale);   // the first token's two words, the second one's
+    // lanes of even numbers keep the first token and get the other half of its channels, the others the second one
+    const bool odd = threadIdx.x & 1;
+    const unsigned give0 = odd ? kc[0] : kc[2], give1 = odd ? kc[1] : kc[3];
+    const unsigned get0 = (unsigned)__builtin_amdgcn_update_dpp(0, (int)give0, 0xB1, 0xf, 0xf, true);   // quad_perm 1,0,3,2
+    const unsigned get1 = (unsigned)__builtin_amdgcn_update_dpp(0, (int)give1, 0xB1, 0xf, 0xf, true);
+    kc = odd ? u32x4{get0, get1, kc[2], kc[3]} : u32x4{kc[0], kc[1], get0, get1};
+    // V: from channel after channel of a token to token after token of a channel
+    if constexpr (E == 4) {
+      unsigned a[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) a[i] = encode4<WILD>(v[VW * i], v[VW * i + VW - 1], v_scale);
+      const unsigned low01 = __builtin_amdgcn_perm(a[1], a[0], 0x05010400u), high01 = __builtin_amdgcn_perm(a[1], a[0], 0x07030602u);
+      const unsigned low23 = __builtin_amdgcn_perm(a[3], a[2], 0x05010400u), high23 = __builtin_amdgcn_perm(a[3], a[2], 0x07030602u);
+      vc[0] = __builtin_amdgcn_perm(low23, low01, 0x05040100u);
+      vc[1] = __builtin_amdgcn_perm(low23, low01, 0x07060302u);
+      vc[E - 2] = __builtin_amdgcn_perm(high23, high01, 0x05040100u);
+      vc[E - 1] = __builtin_amdgcn_perm(high23, high01, 0x07060302u);
+    } else {
+      const unsigned w01 = encode4<WILD>(v[0], v[1], v_scale), w23 = encode4<WILD>(v[2], v[3], v_scale);
+      vc[0] = __builtin_amdgcn_perm(w23, w01, 0x06040200u);
+      vc[E - 1] = __builtin_amdgcn_perm(w23, w01, 0x07050301u);
+    }
+  }
+
+  // top: of the whole block, the finite ones'; wild: the thread has others
+  __device__ __forceinline__ void store(const Place& x, const unsigned (&top)[2], bool wild, bool begun, char* k_codes, char* v_codes, unsigned char* scales) {
+    const int tid = threadIdx.x % kThreads;
+    int s[2];
+#pragma unroll
+    for (int kv = 0; kv < 2; ++kv) s[kv] = max(scale_for(top[kv]), had[kv]);
+    if (__builtin_expect(max(top[0], top[1]) > kTopBits, 0)) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) k[i] = at_most_top(k[i] & 0xffffu) | at_most_top(k[i] >> 16) << 16;
+#pragma unroll
+      for (int i = 0; i < 4 * VW; ++i) v[i] = at_most_top(v[i] & 0xffffu) | at_most_top(v[i] >> 16) << 16;
+    }
+    u32x4 kc;
+    unsigned vc[E];
+    if (__builtin_expect(__any(wild), 0)) encode<true>(kc, vc, as_scale(s[0]), as_scale(s[1]));
+    else encode<false>(kc, vc, as_scale(s[0]), as_scale(s[1]));
+    u32x4* const k_to = reinterpret_cast<u32x4*>(k_codes + x.k_at);
+    unsigned* const v_to = reinterpret_cast<unsigned*>(v_codes + x.v_at);
+    if constexpr (ALL) {
+      if (!SOME || x.own_k) *k_to = kc;
+#pragma unroll
+      for (int e = 0; e < E; ++e) v_to[256 * e] = vc[e];
+      if (tid < 2) scales[kFp8VScales * tid] = (unsigned char)(tid == 0 ? s[0] : s[1]);
+    } else {
+      const bool k_grown = !begun && s[0] > had[0], v_grown = !begun && s[1] > had[1];
+      if (x.own_k) {
+        *k_to = kc;
+      } else if (k_grown && x.k_at >= 0) {
+        u32x4 c = *k_to;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) c[i] = again4(c[i], as_scale(had[0]), as_scale(s[0]));
+        *k_to = c;
+      }
+      if (x.has_v || v_grown) {
+        if (x.has_v != 15u) {   // beside bytes of other tokens
+          const unsigned bytes = bytes_of(x.has_v);
+          unsigned was[E];
+#pragma unroll
+          for (int e = 0; e < E; ++e) was[e] = v_to[256 * e];
+#pragma unroll
+          for (int e = 0; e < E; ++e) vc[e] = (vc[e] & bytes) | ((v_grown ? again4(was[e], as_scale(had[1]), as_scale(s[1])) : was[e]) & ~bytes);
+        }
+#pragma unroll
+        for (int e = 0; e < E; ++e) v_to[256 * e] = vc[e];
+      }
+      if (tid < 2 && (begun || (tid == 0 ? k_grown : v_grown))) scales[kFp8VScales * tid] = (unsigned char)(tid == 0 ? s[0] : s[1]);
+    }
+  }
+};
+
+// One block of heads head0, .. < head1, HEADS of them at once. there: which of its tokens have a row (sh.member).
+template <int D, bool ALL, int HEADS>
+__device__ __forceinline__ void store_heads(const RowsParams& p, StoreShared<HEADS>& sh, unsigned there, int slot0, int head0, int head1) {
+  using Part = StorePart<D, ALL>;
+  const int P = 1 << p.page_shift, nth = (slot0 & (P - 1)) / kBlock, tid = threadIdx.x % kThreads, own = HEADS == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / kThreads);
+  const bool begun = there & 1u;
+  const typename Part::Place place = Part::place(p, sh.member, there);
+#pragma unroll 1
+  for (int first = head0, round = 0; first < head1; first += HEADS, round ^= 1) {
+    const int head = min(first + own, head1 - 1);   // (a group that has none left does the last one's again, and does not store it)
+    char* const at = head_of<D>(p, slot0, head);
+    char* const codes = at + nth * (kBlock * D);
+    unsigned char* const scales = (unsigned char*)at + 2 * P * D + nth;
+    Part part;
+    part.load(place, head * p.head_stride, begun, scales);
+    unsigned top[2] = {top_of(part.k), top_of(part.v)};
+    const bool wild = max(top[0], top[1]) >= 0x7f80u;
+    if (__builtin_expect(__any(wild), 0)) {
+      top[0] = finite_top_of(part.k);
+      top[1] = finite_top_of(part.v);
+    }
+#pragma unroll
+    for (int kv = 0; kv < 2; ++kv) {
+      top[kv] = (unsigned)wave_max_upto((int)top[kv]);
+      if ((tid & 63) == 63) sh.top[round][own][kv][tid >> 6] = top[kv];
+    }
+    __syncthreads();   // (one a round: the next one's maxima are in the other place)
+#pragma unroll
+    for (int kv = 0; kv < 2; ++kv) {
+      top[kv] = 0;
+#pragma unroll
+      for (int w = 0; w < kThreads / 64; ++w) top[kv] = max(top[kv], sh.top[round][own][kv][w]);
+    }
+    if (first + own < head1) part.store(place, top, wild, begun, codes, codes + P * D, scales);
+  }
+}
+
+// A workgroup looks after `chunk` rows, and has `heads` of their heads.
+template <int D, bool LIST, int HEADS>
+__global__ __launch_bounds__(HEADS * kThreads) void kv_store_paged_fp8_kernel(const RowsParams p, int chunk, int heads, int Hkv) {
+  __shared__ StoreShared<HEADS> sh;
+  const int tid = threadIdx.x, lane = tid & 63, t = tid & (kBlock - 1);
+  const int row0 = blockIdx.y * chunk, row1 = min(row0 + chunk, p.rows), head0 = blockIdx.x * heads, head1 = min(head0 + heads, Hkv);
+  if (tid < kWindow) {
+    const int row = row0 - (kBlock - 1) + tid, slot = row >= 0 && row < p.rows ? p.slots[row] : -1;
+    sh.slot[tid] = (unsigned)slot < (unsigned)p.n_slots ? slot : -1;
+  }
+  __syncthreads();
+  const int mine = lane < row1 - row0 ? sh.slot[kBlock - 1 + lane] : -1;   // (32 at most, the same in every wavefront)
+  for (uint64_t pending = __ballot(mine >= 0); pending;) {
+    const int r = __builtin_ctzll(pending), slot = __builtin_amdgcn_readlane(mine, r), slot0 = slot & -kBlock;
+    pending &= ~__ballot((mine & -kBlock) == slot0);   // (-1 is in no block)
+    // the row of token t, if the block's tokens stand in a row
+    const int place = r + t - (slot - slot0);
+    int other = sh.slot[kBlock - 1 + place] == slot0 + t ? row0 + place : -1;
+    unsigned there = (unsigned)__ballot(other >= 0);
+    if (there != ~0u) {
+      if constexpr (LIST) {
+        const int x = p.row_of[slot0 + t];
+        other = (unsigned)x < (unsigned)p.rows && p.slots[x] == slot0 + t ? x : -1;   // (what no row has written is anything)
+        there = (unsigned)__ballot(other >= 0);
+        if (there == 0) continue;
+      } else {
+        __syncthreads();   // (the last block's members are not needed any more)
+        if (tid < kBlock) sh.member[tid] = INT_MAX;
+        __syncthreads();
+        for (int i = tid; i < p.rows; i += HEADS * kThreads) {
+          const unsigned off = (unsigned)p.slots[i] - (unsigned)slot0;
+          if (off < (unsigned)kBlock) atomicMin(&sh.member[off], i);   // (of a slot that two rows have the first one has it)
+        }
+        __syncthreads();
+        other = sh.member[t];
+        there = (unsigned)__ballot(other != INT_MAX);
+      }
+    }
+    const int leader = __builtin_amdgcn_readlane(other, __builtin_ctz(there));
+    if (leader < row0 || leader >= row1) continue;
+    __syncthreads();   // (nor its maxima)
+    if (tid < kBlock) sh.member[tid] = other;
+    __syncthreads();
+    if (there == ~0u) store_heads<D, true, HEADS>(p, sh, there, slot0, head0, head1);
+    else store_heads<D, false, HEADS>(p, sh, there, slot0, head0, head1);
+  }
+}
+
+template <int D>
+void launch_store(const RowsParams& p, int Hkv, bool list, hipStream_t stream) {
+  // few rows: one a workgroup, one head each; more: as many of both as leave workgroups enough
+  const int64_t row_heads = (int64_t)p.rows * Hkv;
+  int chunk = 1;
+  while (chunk < kMostChunk && row_heads / chunk > kEnoughWorkgroups) chunk *= 2;
+  const int64_t each = row_heads / chunk / kEnoughWorkgroups;
+  const bool one = each < kHeadsAtOnce;
+  const int heads = one ? 1 : (int)(each < kMostHeads ? each : kMostHeads) / kHeadsAtOnce * kHeadsAtOnce;
+  const dim3 grid((unsigned)((Hkv + heads - 1) / heads), (unsigned)((p.rows + chunk - 1) / chunk)), threads((one ? 1 : kHeadsAtOnce) * kThreads);
+  if (one && list) hipLaunchKernelGGL((kv_store_paged_fp8_kernel<D, true, 1>), grid, threads, 0, stream, p, chunk, heads, Hkv);
+  else if (one) hipLaunchKernelGGL((kv_store_paged_fp8_kernel<D, false, 1>), grid, threads, 0, stream, p, chunk, heads, Hkv);
+  else if (list) hipLaunchKernelGGL((kv_store_paged_fp8_kernel<D, true, kHeadsAtOnce>), grid, threads, 0, stream, p, chunk, heads, Hkv);
+  else hipLaunchKernelGGL((kv_store_paged_fp8_kernel<D, false, kHeadsAtOnce>), grid, threads, 0, stream, p, chunk, heads, Hkv);
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -266,7 +392,7 @@ __global__ __launch_bounds__(kThreads) void kv_load_paged_fp8_kernel(const RowsP
       if ((unsigned)from < (unsigned)p.n_slots) {
         const char* base = head_of<D>(p, from, head);
         const int t = from & (P - 1), nth = t / kBlock;
-        const u32x4 c = *reinterpret_cast<const u32x4*>(base + nth * (kBlock * D) + k_code_at<D>(t % kBlock, piece * 16));
+        const u32x4 c = *reinterpret_cast<const u32x4*>(base + nth * (kBlock * D) + k_code_at(t % kBlock, piece * 16));
         const float scale = as_scale(((const unsigned char*)base)[2 * P * D + nth]);
         const u32x2 a = decode4(c[0], scale), b = decode4(c[1], scale), d = decode4(c[2], scale), e = decode4(c[3], scale);
         lo = u32x4{a[0], a[1], b[0], b[1]};
@@ -350,7 +476,7 @@ fspad_status check_geometry(const fspad_paged_desc* desc, int32_t rows) {
   return FSPAD_OK;
 }
 
-constexpr int kMaxStoreRows = 65535 * kChunk;   // (a launch's second dimension)
+constexpr int kMaxStoreRows = 1048560;
 
 }  // namespace
 
@@ -376,17 +502,9 @@ extern "C" fspad_status fspad_kv_store_paged_byte(const fspad_paged_desc* desc, 
   RowsParams p = rows_params(*desc, rows, const_cast<void*>(k), const_cast<void*>(v), row_stride, head_stride, slots, pages);
   p.row_of = static_cast<int32_t*>(workspace);
   hipStream_t stream = reinterpret_cast<hipStream_t>(hip_stream);
-  const unsigned heads = (unsigned)desc->n_kv_heads;
-  if (need == 0) {
-    const dim3 grid(heads, (unsigned)rows);
-    if (desc->head_dim == 128) hipLaunchKernelGGL((kv_store_paged_fp8_kernel<128, true>), grid, dim3(kThreads), 0, stream, p);
-    else hipLaunchKernelGGL((kv_store_paged_fp8_kernel<64, true>), grid, dim3(kThreads), 0, stream, p);
-  } else {
-    hipLaunchKernelGGL(kv_rows_of_slots_kernel, dim3((unsigned)((rows + kThreads - 1) / kThreads)), dim3(kThreads), 0, stream, p);
-    const dim3 grid(heads, (unsigned)((rows + kChunk - 1) / kChunk));
-    if (desc->head_dim == 128) hipLaunchKernelGGL((kv_store_paged_fp8_kernel<128, false>), grid, dim3(kThreads), 0, stream, p);
-    else hipLaunchKernelGGL((kv_store_paged_fp8_kernel<64, false>), grid, dim3(kThreads), 0, stream, p);
-  }
+  if (need > 0) hipLaunchKernelGGL(kv_rows_of_slots_kernel, dim3((unsigned)((rows + kThreads - 1) / kThreads)), dim3(kThreads), 0, stream, p);
+  if (desc->head_dim == 128) launch_store<128>(p, desc->n_kv_heads, need > 0, stream);
+  else launch_store<64>(p, desc->n_kv_heads, need > 0, stream);
   return hipGetLastError() == hipSuccess ? FSPAD_OK : FSPAD_ERR_HIP;
 }
 

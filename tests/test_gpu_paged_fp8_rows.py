@@ -70,7 +70,7 @@ def _store_and_check(k, v, slots, pool, D, P):
 
 
 @pytest.mark.parametrize("rows,Hkv,D,P", [(1, 1, 64, 32), (1, 1, 128, 32), (17, 3, 64, 32), (33, 5, 128, 64), (16, 1, 128, 256), (47, 2, 64, 256), (9, 52, 128, 32),
-                                          (100, 2, 128, 64), (1024, 1, 64, 64), (1025, 1, 64, 64), (1100, 2, 128, 32), (2000, 1, 128, 256)])
+                                          (100, 2, 128, 64), (1024, 1, 64, 64), (1025, 1, 64, 64), (1100, 2, 128, 32), (2000, 1, 128, 256), (17000, 1, 64, 64)])
 @pytest.mark.parametrize("order", ["in a row", "scattered", "from a block on"])
 def test_store_then_load(rows, Hkv, D, P, order):
     rng = np.random.default_rng(rows + D)
@@ -108,7 +108,7 @@ def test_token_by_token(D, P, spread):
 def test_rows_of_a_block_anywhere_in_a_call():
     """Two sequences' tokens interleaved, backwards and between rows that go nowhere, by the scan and by the list."""
     D, P, rng = 128, 64, np.random.default_rng(2)
-    for rows in (200, 3000):
+    for rows in (200, 3000, 20000):
         slots = np.full(rows, -1, np.int32)
         places = rng.permutation(rows)[:150]
         slots[places] = np.concatenate([np.arange(40, 115), np.arange(64 * 4 + 74, 64 * 4 - 1, -1)])

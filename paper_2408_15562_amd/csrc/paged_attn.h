@@ -128,15 +128,16 @@ __device__ __forceinline__ int piece_length(const CutArgs& p, int blocks, int un
 }
 
 // The pieces of this workgroup. Units are numbered sequence by sequence, head by head, group by group, and behind a sequence's others those
-// without nodes; workgroups eight apart, which share a die and its L2 cache, take neighbouring pieces or windows.
+// without nodes (HEADS_FIRST: head by head, sequence by sequence, group by group); workgroups eight apart, which share a die and its L2 cache, take
+// neighbouring pieces or windows.
 struct Piece {
   int b, g, y, len, n, half, begin, end, index, count;   // blocks [begin, end) of a unit; index: its slot; count: pieces of the unit
   bool dead;
 };
 // LINES: windows may be what the call is cut into; SLABS: workgroups have two of them, or one.
-template <bool LINES, bool SLABS>
+template <bool LINES, bool SLABS, bool HEADS_FIRST>
 struct Cutter {
-  int lane, most, window, length;   // length: of the line of units, in pieces or in blocks
+  int lane, most, window, length;   // length: of the line of units, in pieces or in blocks (HEADS_FIRST: of one head's)
   int2 seq;                 // 64 sequences at a time, one a lane, from `first` on: length and nodes
   int first, before, in_these;   // the line's length before theirs, and theirs
   int at, stop, step;       // this workgroup's next place on the line; the end and the step of them
@@ -155,7 +156,7 @@ struct Cutter {
     int tail = c.unit;
     if (SLABS && c.s.half && !p.uncut) tail = by_pieces() ? (blocks + most - 1) / most : blocks + p.piece_cost;
     c.head = c.s.live == 0 ? 0 : (c.s.live - 1) * c.unit + tail;
-    c.own = first + lane < p.B ? p.Hkv * (c.head + (p.groups - c.s.live) * dead_length(p)) : 0;
+    c.own = first + lane < p.B ? (HEADS_FIRST ? 1 : p.Hkv) * (c.head + (p.groups - c.s.live) * dead_length(p)) : 0;
     c.upto = wave_sum_upto(c.own);
     return c;
   }
@@ -183,26 +184,28 @@ struct Cutter {
       if (first + 64 >= p.B) break;
     }
     before = length - in_these;
+    const int all = HEADS_FIRST ? p.Hkv * length : length;
     // (the grid is a multiple of eight)
     const int die = blockIdx.x & 7, nth = blockIdx.x >> 3, of_die = gridDim.x >> 3;
     if (by_pieces()) {
-      const int share = (length + 7) >> 3;
+      const int share = (all + 7) >> 3;
       at = die * share + nth;
-      stop = min((die + 1) * share, length);
+      stop = min((die + 1) * share, all);
       step = of_die;
     } else {
       const int wgs = (int)gridDim.x, nth_window = die * of_die + nth;
-      window = __builtin_amdgcn_readfirstlane((length + wgs - 1) / wgs);
+      window = __builtin_amdgcn_readfirstlane((all + wgs - 1) / wgs);
       const int64_t begin = (int64_t)nth_window * window;
-      at = (int)(begin < length ? begin : length);
-      stop = (int)(begin + window < length ? begin + window : length);
+      at = (int)(begin < all ? begin : all);
+      stop = (int)(begin + window < all ? begin + window : all);
       step = 0;
     }
   }
   // the next piece of this workgroup, if there is one
   __device__ __forceinline__ bool next(const CutArgs& p, Piece& r) {
     while (at < stop) {
-      if (at < before || at >= before + in_these) {   // of other 64 sequences
+      const int of_head = HEADS_FIRST ? __builtin_amdgcn_readfirstlane(at / length) : 0, place = at - of_head * length;
+      if (place < before || place >= before + in_these) {   // of other 64 sequences
         before = in_these = 0;
         first = -64;
         do {
@@ -210,22 +213,22 @@ struct Cutter {
           first += 64;
           seq = seq_at(p, first + lane);
           in_these = last_lane(count(p).upto);
-        } while (at >= before + in_these);
+        } while (place >= before + in_these);
       }
       const Counts c = count(p);
-      const int i = __builtin_ctzll(__ballot(at < before + c.upto));   // the sequence that the place lies in
+      const int i = __builtin_ctzll(__ballot(place < before + c.upto));   // the sequence that the place lies in
       r.b = first + i;
       r.len = __builtin_amdgcn_readlane(c.s.len, i);
       r.n = __builtin_amdgcn_readlane(c.s.n, i);
       const int unit = __builtin_amdgcn_readlane(c.unit, i), head = __builtin_amdgcn_readlane(c.head, i);
       const int nb = __builtin_amdgcn_readlane(c.s.nb, i), live = __builtin_amdgcn_readlane(c.s.live, i);
-      const int rel = at - before - __builtin_amdgcn_readlane(c.upto - c.own, i);
-      r.dead = rel >= p.Hkv * head;
+      const int rel = place - before - __builtin_amdgcn_readlane(c.upto - c.own, i), heads = HEADS_FIRST ? 1 : p.Hkv;
+      r.dead = rel >= heads * head;
       r.count = 1;
       r.begin = r.end = r.index = r.half = 0;
       int taken = step;
       if (__builtin_expect(r.dead, 0)) {
-        const int others = p.groups - live, x = rel - p.Hkv * head, u = x / dead_length(p), off = x - u * dead_length(p);
+        const int others = p.groups - live, x = rel - heads * head, u = x / dead_length(p), off = x - u * dead_length(p);
         r.g = u / others;
         r.y = live + u - r.g * others;
         if (!by_pieces()) {
@@ -261,6 +264,7 @@ struct Cutter {
           r.index = 2 * own + (r.begin == 0 ? 1 : 0);
         }
       }
+      if (HEADS_FIRST) r.g += of_head;
       // (quotients come from the vector unit: what follows is the same in all lanes)
       r.g = __builtin_amdgcn_readfirstlane(r.g);
       r.y = __builtin_amdgcn_readfirstlane(r.y);
@@ -408,7 +412,7 @@ void tree_attn_paged_kernel(const PagedParams) {
     asm volatile("" :: "s"(line1), "s"(line2), "s"(line3));
   }
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  using Cuts = Cutter<(Form::ROWS > 16), (D == 128 && Form::ROWS == 32)>;
+  using Cuts = Cutter<(Form::ROWS > 16), (D == 128 && Form::ROWS == 32), Form::HEADS_FIRST>;
   Cuts cutter(cut_args(p), threadIdx.x & 63);
   Piece piece;
   for (bool again = false; cutter.next(cut_args(p), piece); again = true) {

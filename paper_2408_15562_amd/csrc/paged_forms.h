@@ -191,6 +191,7 @@ struct Form16 {
   struct Values {
     unsigned c[D / 16], scale[2];
   };
+  static constexpr bool HEADS_FIRST = false;   // the order of a call's units
   // where a block's codes and scales start in a head's part of a page, in which a lane's Offsets are counted
   __device__ static constexpr int head_bytes(int P) { return page_head_bytes(D, P); }
   __device__ static __forceinline__ unsigned block_codes(unsigned in_page) { return in_page * (D / 2); }
@@ -443,6 +444,7 @@ struct Form32 {
   struct Values {
     unsigned c[4 * KB], scale[4];   // eight of the lane's 16 keys, the scales of all
   };
+  static constexpr bool HEADS_FIRST = false;   // the order of a call's units
   // where a block's codes and scales start in a head's part of a page, in which a lane's Offsets are counted
   __device__ static constexpr int head_bytes(int P) { return page_head_bytes(D, P); }
   __device__ static __forceinline__ unsigned block_codes(unsigned in_page) { return in_page * (D / 2); }

@@ -31,7 +31,7 @@ __device__ __forceinline__ unsigned bytes_of(unsigned bits) { return (((bits & 1
 // What both forms share: one scale byte of K and one of V a block.
 template <int D>
 struct Fp8Block {
-  static constexpr int kCodes = kFp8BlockTokens * D;   // of a block, K's or V's
+  static constexpr bool HEADS_FIRST = true;
   __device__ static constexpr int head_bytes(int P) { return page_head_bytes_fp8(D, P); }
   __device__ static __forceinline__ unsigned block_codes(unsigned in_page) { return in_page * D; }
   __device__ static __forceinline__ unsigned block_scales(unsigned in_page) { return in_page / kFp8BlockTokens; }
@@ -45,6 +45,7 @@ template <int D>
 struct Form16Fp8 : Form16<D, true>, Fp8Block<D> {
   using Base = Form16<D, true>;
   using Block = Fp8Block<D>;
+  using Block::HEADS_FIRST;
   using Block::head_bytes;
   using Block::block_codes;
   using Block::block_scales;
@@ -126,6 +127,7 @@ template <int D, int TILES>
 struct Form32Fp8 : Form32<D, TILES, true>, Fp8Block<D> {
   using Base = Form32<D, TILES, true>;
   using Block = Fp8Block<D>;
+  using Block::HEADS_FIRST;
   using Block::head_bytes;
   using Block::block_codes;
   using Block::block_scales;

@@ -1,7 +1,16 @@
 // Tree-masked attention over a paged 8-bit cache (arXiv 2408.15562, Preliminaries, validation phase, as fspad_attn.hip; the cache format is in
 // include/fspad.h). gfx950 (CDNA4) only.
 //
-// The kernel of paged_attn.h on the forms of paged_forms_fp8.h.
+// The kernel of paged_attn.h on the forms of paged_forms_fp8.h. A block of 32 keys takes a wavefront of 32 rows (D = 128) 93 vector instructions and 16 products
+// (540 clocks), against 155 and 16 of the 4-bit cache: the pages hold V's codes key after key, so that nothing is turned.
+//
+// What bounds it. Single tokens: memory. 64 sequences of 4000 tokens, 8 kv heads of D = 64 (262 MB), 49 us; 32 of them, D = 128, 50 us, 16384 tokens 188 us: 5.3 to 5.7 TB/s, 5.9 for
+// longer ones. Trees on grouped heads: products and vector instructions, which do not hide each other here (64 on 8 kv heads, 60 nodes, 16384 tokens: 45 us, 730 TFLOP/s; 28 more for 16384 more,
+// 1140 TFLOP/s; the same without any loads). The matrix cores are busy for 44 % of a SIMD's clocks, the vector unit for 62. Trees on heads of their own: both (4 sequences of 4096 tokens, 60 nodes and 52 heads,
+// 231 MB: 59 us, 45 without loads). Of each, 6 (a token) to 11 us (trees) are starts, merges and joins.
+// Tried at the last two, and not kept: exponentials and conversions between the products by scheduling groups, eight ways (60.3 to 61.0 for 60.9 us and 45.3 to 47.6 for 46.6);
+// loads two turns ahead (16 rows, one token 8.8 -> 9.3 us, 32 tokens of 4000 51.1 -> 49.9; 32 rows of D = 128 spill); loads past the caches (59 -> 69 and 46 -> 58).
+// Units go head by head: every die then has some heads of all sequences instead of all heads of some, whose lengths differ (16 ragged trees 73.0 -> 69.6 us).
 #include <hip/hip_runtime.h>
 #include <stddef.h>
 #include <stdint.h>

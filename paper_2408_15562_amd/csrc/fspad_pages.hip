@@ -62,7 +62,7 @@ __device__ __forceinline__ void along_row(const int32_t* row, int n, Fn&& fn) {
 }
 
 // How `shared` changes: a workgroup counts in LDS what happens to its own pages, for which it looks through all entries that the call is about. No
-// atomics on memory: 50000 of them took 50 us (1024 rows of 31 to 250 pages, half of them released), the look takes 7.
+// atomics on memory: 70000 of them took 50 us (1024 rows of 31 to 250 pages, half of them released), the look takes 14, and 3.5 in a call of a few rows.
 
 // ---------------------------------------------------------------------------------------------
 // Fork.
@@ -386,7 +386,7 @@ __global__ __launch_bounds__(kThreads) void page_compact_kernel(const CompactPar
 __global__ __launch_bounds__(kThreads) void page_compact_stack_kernel(const CompactParams p) { new_stack(p, min(max(*p.n_free, 0), p.n_pages)); }
 
 // ---------------------------------------------------------------------------------------------
-// Copies. Memory-bound: a workgroup takes 16 KB of a pair at a time.
+// Copies. Memory-bound: a workgroup takes 16 KB of a pair at a time. 910 pages of 131 KB (240 MB read and written) in 47 us, 5.1 TB/s.
 struct CopyParams {
   char* pages;
   const int32_t* src;

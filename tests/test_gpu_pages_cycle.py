@@ -1,6 +1,9 @@
 """Shared pages and the paged caches together, as a server makes the calls that answers each prompt several times: prompts get pages and are
 stored, are forked, every branch goes its own way (attention, new pages, stores), some end, the pool is compacted. In 8-bit pages and in 4-bit ones,
 two layers interleaved in one pool; every step against the oracle; then a step of all of it captured into a graph, and calls on two streams at once."""
+import os
+import re
+
 import numpy as np
 import pytest
 import torch
@@ -245,3 +248,27 @@ def test_calls_on_two_streams_at_once():
         flat = [t for r in got[side] for t in (r if isinstance(r, tuple) else (r,))]
         for a, b in zip(flat, alone[side]):
             assert torch.equal(a, b)
+
+
+def test_the_documented_calls():
+    """README's lines about shared pages, as they stand there."""
+    with open(os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "README.md")) as f:
+        block = next(b for b in re.findall(r"```python\n(.*?)```", f.read(), re.S) if "fspad_page_fork" in b)
+    s = Server(True, 4, 1, 2, 1, 128, 32, width=5, n_pages=14, seed=2)
+    s.grow([101, 40, 0, 0])
+    parts = re.split(r"(?m)^# ", block)
+    ns = dict(torch=torch, fspad=fspad, i32=dict(dtype=torch.int32, device=DEV), n_pages=14, P=32, table=s.table, free=s.free, n_free=s.n_free, kv_len=s.kv_len, pages=s.pool)
+    h = s.host
+    exec(parts[0], ns)
+    s.shared = ns["shared"]
+    cs, cd, h["kv_len"], h["n_free"], h["shared"], granted, h["table"] = pages.fork([0, 0], [2, 3], h["kv_len"], h["table"], h["free"], h["n_free"], h["shared"], 32)
+    s._copied(cs, cd)
+    assert granted.all() and ns["granted"].tolist() == [1, 1]
+    s.attend()
+    exec("# " + parts[1], ns)
+    h["kv_len"], h["n_free"], h["shared"], h["free"] = pages.release([0, 0, 1, 0], h["kv_len"], h["table"], h["free"], h["n_free"], h["shared"], 32)
+    s.same_state()
+    exec("# " + parts[2], ns)
+    cs, cd, h["table"], h["free"], h["shared"] = pages.compact(h["kv_len"], h["table"], h["free"], h["n_free"], h["shared"], 32)
+    s._copied(cs, cd)
+    s.attend()

@@ -544,7 +544,7 @@ size_t fspad_kv_page_bytes_byte(int32_t n_kv_heads, int32_t head_dim, int32_t pa
  *             call (what the block holds of it then is not specified)
  *   rows      0..1048560; 0 does nothing (no pointer is looked at)
  *   pages     dev, 16-byte aligned. Tokens of other blocks stay as they are; no other call may use a block that this one stores to meanwhile
- *   workspace dev, 16-byte aligned, >= fspad_kv_store_paged_byte_workspace_bytes(desc, rows): 0 up to 16384 rows (may be NULL then), 4 bytes a
+ *   workspace dev, 16-byte aligned, >= fspad_kv_store_paged_byte_workspace_bytes(desc, rows): 0 up to 2048 rows (may be NULL then), 4 bytes a
  *             slot of the pool for more; contents ignored on entry, undefined on exit; two calls that may overlap in time need different ones
  * Reads n_kv_heads, head_dim, io_dtype, page_tokens, n_pages and page_stride of the descriptor, as fspad_kv_load_paged_byte does.
  */
@@ -595,7 +595,7 @@ fspad_status fspad_tree_attn_paged_byte(const fspad_paged_desc* desc,
  * A fork is refused, granted[f] = 0 with nothing changed for it, if src[f] or dst[f] is outside [0,B), or they are the same, if row dst[f] has tokens or a fork
  * before f in the call names it too (refused or not), if n_tokens[f] is below zero, above kv_len[src[f]], or more than a row holds, or if it needs a page and there
  * are as many forks before it that need one (refused for lack of pages or not, but not those refused for another reason) as the stack has.
- *   n_forks     1..2048;  src, dst dev [n_forks] i32;  n_tokens dev [n_forks] i32, NULL: all tokens of src
+ *   n_forks     0..2048;  src, dst dev [n_forks] i32;  n_tokens dev [n_forks] i32, NULL: all tokens of src
  *   copy_src, copy_dst, granted   dev [n_forks] i32 out;  n_free_out dev [1] out;  shared_out dev [n_pages] out
  * No workspace. The stack itself is not written to.
  */

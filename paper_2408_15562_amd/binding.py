@@ -900,7 +900,7 @@ def fspad_kv_store_paged_byte_workspace_bytes(desc: fspad_paged_desc, rows: int)
 def fspad_kv_store_paged_byte(k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, pages: torch.Tensor, workspace: Optional[torch.Tensor] = None,
                              stream=None, prepare: bool = False):
     """fspad_kv_store_paged into 8-bit pages. A call that stores the first token of a block of 32 begins the block; to other blocks it
-    adds. `workspace`: 4 bytes a slot of the pool, for more than 16384 rows. Returns pages; with prepare=True a PreparedCall."""
+    adds. `workspace`: 4 bytes a slot of the pool, for more than 2048 rows. Returns pages; with prepare=True a PreparedCall."""
     rows, Hkv, D, (row_stride, head_stride) = _paged_rows(k, v, slots)
     desc = _pool_desc(pages, D, fp8=True)
     if pages.shape[1] != Hkv:

@@ -87,9 +87,13 @@ __device__ __forceinline__ unsigned again4(unsigned codes, float had, float scal
 //
 // Groups of 256 threads have a head each. Every thread has a piece of K and of V the channels of four neighbouring tokens that make four neighbouring bytes of
 // D/32 places: what it rounds it stores, whole lines a wavefront.
-constexpr int kScanRows = 16384;   // at most, without the list
+// At most, without the list. Rows of trees of 60 nodes, 5 of them stored, 8 heads, both ways: 3840 rows 9.8 us without and 8.0 with it, 15360 35.6 and 14.7; a prompt of 8191 rows of 32 heads 90
+// either way.
+constexpr int kScanRows = 2048;
 constexpr int kMostChunk = 32;     // rows that a workgroup looks after
 constexpr int kWindow = kMostChunk + 2 * (kBlock - 1);   // and sees
+// Rows are taken together down to so many workgroups. 1024, 2048, 4096: accepted paths of 4 trees, 52 heads (with their load) 8.5, 8.9, 9.7 us; a token of 512 sequences, 8 heads, 14.7, 13.5, 11.6
+constexpr int kChunkWorkgroups = 2048;
 constexpr int kEnoughWorkgroups = 1024, kHeadsAtOnce = 2, kMostHeads = 4;
 
 __global__ __launch_bounds__(kThreads) void kv_rows_of_slots_kernel(const RowsParams p) {
@@ -359,7 +363,7 @@ void launch_store(const RowsParams& p, int Hkv, bool list, hipStream_t stream) {
   // few rows: one a workgroup, one head each; more: as many of both as leave workgroups enough
   const int64_t row_heads = (int64_t)p.rows * Hkv;
   int chunk = 1;
-  while (chunk < kMostChunk && row_heads / chunk > kEnoughWorkgroups) chunk *= 2;
+  while (chunk < kMostChunk && row_heads / chunk > kChunkWorkgroups) chunk *= 2;
   const int64_t each = row_heads / chunk / kEnoughWorkgroups;
   const bool one = each < kHeadsAtOnce;
   const int heads = one ? 1 : (int)(each < kMostHeads ? each : kMostHeads) / kHeadsAtOnce * kHeadsAtOnce;

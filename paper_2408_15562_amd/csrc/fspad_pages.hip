@@ -438,9 +438,9 @@ extern "C" fspad_status fspad_page_fork(int32_t B, int32_t page_tokens, int32_t 
                                         int32_t* copy_src, int32_t* copy_dst, int32_t* kv_len_out, int32_t* n_free_out,
                                         int32_t* shared_out, int32_t* granted, void* hip_stream) {
   if (const fspad_status st = check_table(B, page_tokens, n_pages, table_width, table_stride)) return st;
-  if (n_forks < 1 || n_forks > kMaxRows) return FSPAD_ERR_SHAPE;
-  if (!src || !dst || !kv_len || !block_table || !free_pages || !n_free || !shared || !copy_src || !copy_dst || !kv_len_out || !n_free_out || !shared_out || !granted)
-    return FSPAD_ERR_NULL;
+  if (n_forks < 0 || n_forks > kMaxRows) return FSPAD_ERR_SHAPE;
+  if (!kv_len || !block_table || !free_pages || !n_free || !shared || !kv_len_out || !n_free_out || !shared_out) return FSPAD_ERR_NULL;
+  if (n_forks > 0 && (!src || !dst || !copy_src || !copy_dst || !granted)) return FSPAD_ERR_NULL;
   const int tiles = (n_pages + kTile - 1) / kTile;
   // a workgroup for every tile, and for some sixteen thousand entries that forks may copy
   const bool alone = tiles <= kAloneTiles && (int64_t)n_forks * table_width <= 4 * kTile;
@@ -498,9 +498,6 @@ extern "C" fspad_status fspad_page_compact(int32_t B, int32_t page_tokens, int32
                            log2_of(page_tokens), n_pages, table_width, words};
   hipStream_t stream = reinterpret_cast<hipStream_t>(hip_stream);
   const unsigned lds = (unsigned)(2 * words * sizeof(int));
-  if (lds > 65536)
-    for (const void* kernel : {reinterpret_cast<const void*>(page_compact_kernel<true>), reinterpret_cast<const void*>(page_compact_kernel<false>)})
-      if (hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, kMaxPages / 4) != hipSuccess) return FSPAD_ERR_HIP;
   const int64_t entries = (int64_t)B * table_width;
   const unsigned wgs = (unsigned)workgroups(entries > n_pages ? entries : n_pages, kThreads, 256);
   if (free_out != free_pages || wgs == 1) {

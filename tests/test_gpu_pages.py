@@ -100,6 +100,16 @@ def test_fork(B, P, n_pages, width, place):
         table.copy_(before)
 
 
+@pytest.mark.parametrize("B,n_pages,width", [(3, 50, 4), (300, 40000, 60)])
+def test_no_forks(B, n_pages, width):
+    s = State(1, B, 16, n_pages, width)
+    lens, table, free, n_free, shared = s.args()
+    before = table.clone()
+    got = fspad.fspad_page_fork(_dev([]), _dev([]), lens, table, free, n_free, shared, 16)
+    torch.cuda.synchronize()
+    assert got[0].numel() == 0 and torch.equal(table, before) and torch.equal(got[2], lens) and torch.equal(got[3], n_free) and torch.equal(got[4], shared)
+
+
 @pytest.mark.parametrize("B,P,n_pages,width", SIZES)
 @pytest.mark.parametrize("place", ["apart", "in place", "bad entries"])
 @pytest.mark.parametrize("part", [0.0, 0.4, 1.0])

@@ -66,8 +66,8 @@ def test_store_and_load_refuse_arguments(lib):
 
 def test_store_of_many_rows_needs_a_workspace(lib):
     d = _desc()
-    assert [fspad.fspad_kv_store_paged_byte_workspace_bytes(d, r) for r in (0, 1, 16384, 16385, 90000)] == [0, 0, 0, 1280, 1280]
-    call = lambda ws, n: lib.fspad_kv_store_paged_byte(ctypes.byref(d), 16385, P16, P16, 256, 128, P16, P16, ws, n, None)  # noqa: E731
+    assert [fspad.fspad_kv_store_paged_byte_workspace_bytes(d, r) for r in (0, 1, 2048, 2049, 90000)] == [0, 0, 0, 1280, 1280]
+    call = lambda ws, n: lib.fspad_kv_store_paged_byte(ctypes.byref(d), 2049, P16, P16, 256, 128, P16, P16, ws, n, None)  # noqa: E731
     assert call(None, 1280) == WORKSPACE and call(P16, 1279) == WORKSPACE and call(P16 + 8, 1280) == WORKSPACE
 
 

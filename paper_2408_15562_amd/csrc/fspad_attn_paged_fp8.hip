@@ -10,6 +10,8 @@
 // 231 MB: 59 us, 45 without loads). Of each, 6 (a token) to 11 us (trees) are starts, merges and joins.
 // Tried at the last two, and not kept: exponentials and conversions between the products by scheduling groups, eight ways (60.3 to 61.0 for 60.9 us and 45.3 to 47.6 for 46.6);
 // loads two turns ahead (16 rows, one token 8.8 -> 9.3 us, 32 tokens of 4000 51.1 -> 49.9; 32 rows of D = 128 spill); loads past the caches (59 -> 69 and 46 -> 58).
+// Many sequences: wavefronts with rows for themselves (256 single tokens of 100 tokens, 32 on 8 heads 36 -> 19 us; 64 trees of 60 nodes, 500 tokens, D = 64 70 -> 41; of 2000, D = 128 249 -> 168), by the
+// rule at paged_slabs.
 // Units go head by head: every die then has some heads of all sequences instead of all heads of some, whose lengths differ (16 ragged trees 73.0 -> 69.6 us).
 #include <hip/hip_runtime.h>
 #include <stddef.h>
@@ -25,6 +27,11 @@ namespace {
 
 template <int D>
 void launch_rows(const PagedPlan& pl, const PagedParams& p, hipStream_t stream) {
+  if (pl.slabs) {
+    if (pl.rows_per_wave == 16) launch<Form16Fp8<D>, 1, true, false>(pl, p, stream);
+    else pl.slabs == 1 ? launch<Form32Fp8<D, 1>, 1, true, false>(pl, p, stream) : launch<Form32Fp8<D, 1>, 4, true, false>(pl, p, stream);
+    return;
+  }
   if (pl.rows_per_wave == 16) pl.waves == 4 ? launch<Form16Fp8<D>, 4, true>(pl, p, stream) : launch<Form16Fp8<D>, 8, true>(pl, p, stream);
   else if (pl.rows_per_wave == 32) pl.waves == 4 ? launch<Form32Fp8<D, 1>, 4, true>(pl, p, stream) : launch<Form32Fp8<D, 1>, 8, true>(pl, p, stream);
   else if constexpr (D == 64) pl.waves == 4 ? launch<Form32Fp8<64, 2>, 4, true>(pl, p, stream) : launch<Form32Fp8<64, 2>, 8, true>(pl, p, stream);

@@ -397,14 +397,15 @@ struct Places {
   }
 };
 
-// WIDE: a page holds a block's 32 keys (pages of 16 keys: a block's halves lie on two).
-template <class Form, int WAVES, bool WIDE>
+// WIDE: a page holds a block's 32 keys (pages of 16 keys: a block's halves lie on two). SPLIT: a slab has several wavefronts, which split its
+// keys; else a wavefront has a slab, and all keys of the piece, for itself.
+template <class Form, int WAVES, bool WIDE, bool SPLIT>
 __global__ __launch_bounds__(64 * WAVES, WAVES * paged_resident(WAVES, Form::HEAD_DIM, Form::ROWS == 16) / 4)
 void tree_attn_paged_kernel(const PagedParams) {
   Args p = (Args)__builtin_amdgcn_kernarg_segment_ptr();
   constexpr int D = Form::HEAD_DIM, RT = Form::RT, QUADS = Form::QUADS;
-  __shared__ f32x4 merge_o[WAVES][RT * QUADS][64];
-  __shared__ float2 merge_ml[WAVES][RT][64];
+  __shared__ f32x4 merge_o[SPLIT ? WAVES : 1][RT * QUADS][64];
+  __shared__ float2 merge_ml[SPLIT ? WAVES : 1][RT][64];
   {   // (a word of each 64 bytes of the arguments: they come from afar, here all at once instead of line by line where they are used. 0.3 us)
     typedef const __attribute__((address_space(4))) unsigned* Words;
     const unsigned line1 = ((Words)p)[16], line2 = ((Words)p)[32], line3 = ((Words)p)[48];
@@ -412,14 +413,14 @@ void tree_attn_paged_kernel(const PagedParams) {
     asm volatile("" :: "s"(line1), "s"(line2), "s"(line3));
   }
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  using Cuts = Cutter<(Form::ROWS > 16), (D == 128 && Form::ROWS == 32), Form::HEADS_FIRST>;
+  using Cuts = Cutter<(Form::ROWS > 16), (SPLIT && D == 128 && Form::ROWS == 32), Form::HEADS_FIRST>;
   Cuts cutter(cut_args(p), threadIdx.x & 63);
   Piece piece;
   for (bool again = false; cutter.next(cut_args(p), piece); again = true) {
-  if (again) __syncthreads();   // the merge buffers are used again
+  if (SPLIT && again) __syncthreads();   // the merge buffers are used again
   const int lane = (int)here(threadIdx.x & 63);   // (what is made of it is made for every piece)
   const int b = piece.b, g = piece.g, y = piece.y, L = piece.len, n = piece.n;
-  const int ws_shift = piece.half ? 0 : p->ws_shift;
+  const int ws_shift = !SPLIT ? __builtin_ctz(WAVES) : piece.half ? 0 : p->ws_shift;
   const int WS = 1 << ws_shift, KW = WAVES >> ws_shift;   // row slabs, wavefronts that split a slab's keys
   const int slab = wave & (WS - 1), kp = wave >> ws_shift;
   const int row0 = y * p->rows_per_group + slab * Form::ROWS;
@@ -639,6 +640,29 @@ void tree_attn_paged_kernel(const PagedParams) {
   }
   p = fresh(p);
 
+  if constexpr (!SPLIT) {
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+      const RowInfo ri = row_info(t);
+      const float l_row = Form::row_sum(st, t);
+      if (!ri.exists) continue;
+      if (piece.count == 1) {
+        const float inv = l_row == 0.f ? 0.f : 1.0f / l_row;
+#pragma unroll
+        for (int q = 0; q < QUADS; ++q)
+          put_quad(p->out, p->out_bf16, ri.out * D + Form::channel(q, lane), ri.valid ? Form::quad(st, t, q) * inv : f32x4{0.f, 0.f, 0.f, 0.f});
+      } else if (ri.valid) {   // (the join reads no others)
+        float* part = p->part + piece.index * slot_floats<Form>(p->rows_per_group);
+        const int tile = slab * RT + t;
+        if (Form::first_key(lane) == 0)
+          *reinterpret_cast<float2*>(part + (int64_t)p->rows_per_group * D + 2 * (Form::TILE * tile + Form::row(lane))) = make_float2(st.m[t], l_row);
+#pragma unroll
+        for (int q = 0; q < QUADS; ++q) *reinterpret_cast<f32x4*>(part + quad_at<Form>(tile, q, lane)) = Form::quad(st, t, q);
+      }
+    }
+    continue;
+  }
+
   // ---- the key-splitting wavefronts of a slab meet in LDS; each writes its share of the quads
 #pragma unroll
   for (int t = 0; t < RT; ++t) {
@@ -738,11 +762,11 @@ __global__ __launch_bounds__(256) void tree_attn_paged_join_kernel(const PagedPa
   put_quad(p.out, p.out_bf16, (((int64_t)b * p.N + node) * p.Hq + g * p.G + (rr - node * p.G)) * D + Form::channel(quad, lane), acc);
 }
 
-template <class Form, int WAVES, bool WIDE>
+template <class Form, int WAVES, bool WIDE, bool SPLIT = true>
 void launch(const PagedPlan& pl, const PagedParams& p, hipStream_t stream) {
   // a multiple of eight: workgroup w takes places w / 8, one grid's eighth further, .. of die w % 8's share
   const int wgs = pl.max_pieces < pl.resident ? pl.max_pieces : pl.resident;
-  hipLaunchKernelGGL((tree_attn_paged_kernel<Form, WAVES, WIDE>), dim3((unsigned)((wgs + 7) / 8 * 8)), dim3(64 * WAVES), 0, stream, p);
+  hipLaunchKernelGGL((tree_attn_paged_kernel<Form, WAVES, WIDE, SPLIT>), dim3((unsigned)((wgs + 7) / 8 * 8)), dim3(64 * WAVES), 0, stream, p);
   if (!pl.may_cut) return;
   const int rows = pl.rows_per_group < p.N * p.G ? pl.rows_per_group : p.N * p.G;
   hipLaunchKernelGGL((tree_attn_paged_join_kernel<Form>), dim3((unsigned)((rows + Form::TILE - 1) / Form::TILE * (Form::QUADS / 4)), (unsigned)p.Hkv,

@@ -15,7 +15,7 @@ constexpr int kPagedMaxBatch = 1024;
 constexpr int kPagedComputeUnits = 256;
 
 // Workgroups of a compute unit. (Three of four wavefronts, D = 128, would spill: 64 sequences of 2000 tokens, 8 kv heads, 34.2 us, two 30.6.)
-constexpr int paged_resident(int waves, int D, bool rows16) { return waves == 4 ? (rows16 && D == 64 ? 4 : 2) : rows16 && D == 64 ? 2 : 1; }
+constexpr int paged_resident(int waves, int D, bool rows16) { return (rows16 && D == 64 ? 16 : 8) / waves; }
 
 struct PagedPlan {
   int rows_per_wave, WS, waves;   // row slabs and wavefronts of a workgroup (those of a slab split its keys)
@@ -24,6 +24,7 @@ struct PagedPlan {
   int resident;          // workgroups that the device holds at once
   int least_blocks, whole_blocks;   // no piece is shorter, no unit of up to so many blocks is cut
   int piece_cost, join_cost, dead_cost;   // what starting and ending a piece takes, joining pieces, a unit without nodes, in blocks
+  int slabs;             // slabs of a workgroup if a wavefront has all keys of its rows; 0: those of a slab split its keys
   bool may_cut;          // a unit can be so long that it is cut
   bool lines;            // workgroups may take windows of all units: two slots each
   int max_pieces;
@@ -34,18 +35,46 @@ inline int64_t paged_unit_blocks(const fspad_paged_desc& d) {   // at most
   return ((int64_t)d.max_kv_len + kBlockKeys - 1) / kBlockKeys + (d.n_nodes_max + kBlockKeys - 1) / kBlockKeys;
 }
 
+// Whether wavefronts of a call over the 8-bit cache have rows for themselves, with all their keys: a wavefront then starts once for its rows, and nothing
+// is merged. Where there are enough such slabs for the device that is what it costs to start that counts, not how long one takes. 0: they do not; else slabs a workgroup, one,
+// or four where a kv head has more than 64 rows (they read the same keys). Split by four or eight wavefronts / slabs of their own, us; heads are query heads on kv heads:
+//   one token, 32 on 8, D = 128: 64 sequences (512 slabs) of 250 tokens 12.0 / 12.5, 96 of 50 .. 2000 54.5 / 55.6; 128 (1024) of 100 19.2 / 13.1, of 1000 59 / 56, of 50 .. 2000
+//     69 / 70, of 4000 182 / 193; 256 of 100 36 / 19, of 1000 104 / 100. D = 64: 96 of 50 .. 1000 15.3 / 17.7, 256 of 250 24.4 / 17.6, of 50 .. 1000 44 / 38.
+//   7 nodes, 32 on 8, D = 128: 64 (512) of 50 .. 1000 22 / 25, 96 (768) 36 / 35, of 2000 94 / 79, 256 of 500 81 / 64; 192 of 50 .. 4000 186 / 200. D = 64: 64 of 50 .. 1000 14.8 / 19.4, 96
+//     21.4 / 20.4, 256 of 500 53 / 36.
+//   60 nodes, 16 on 16, D = 128: 16 (512) of 1000 22 / 27, 24 (768) 44 / 36, 64 of 500 53 / 47, 64 of 1000 .. 8000 309 / 487.
+//   60 nodes, 32 on 8, D = 128: 8 (512) of 500 17.4 / 20.6, 12 (768) 24 / 21.5, of 2000 59 / 41, of 50 .. 4000 70 / 64, 64 of 500 91 / 70, of 2000 249 / 168. D = 64: 12 of 2000 35 / 31, 64 of 500
+//     70 / 41; four slabs a workgroup 70, one 74 (64 of 500, D = 128), and of 50 .. 4000 222 and 366.
+// More than 32 rows and few keys: the merge takes longer than the keys of one wavefront. One sequence, 60 nodes, 32 on 8, D = 128: one token 11.4 / 10.2, 100 12.1 / 11.7, 250 13.2 / 13.2;
+// 36 nodes on 40 heads, 4 sequences of 100 12.8 / 13.3, of 250 14.0 / 15.2; D = 64, 60 nodes: 1 9.4 / 8.6, 250 12.0 / 11.0, 500 13.5 / 13.5. 7 nodes: 30 tokens 8.6 / 9.1.
+inline int paged_slabs(const fspad_paged_desc& d, int rows, int64_t longest) {
+  const int per_wave = rows <= 16 ? 16 : 32;
+  const int64_t slabs = (int64_t)d.batch * d.n_kv_heads * ((rows + per_wave - 1) / per_wave);
+  const bool many = slabs >= (rows <= 16 ? 4 : 3) * kPagedComputeUnits;
+  if (many && rows > 64) return 4;
+  return (many && longest <= 72) || (rows > 32 && longest <= (d.head_dim == 64 ? 10 : 7)) ? 1 : 0;
+}
+
 // Rows of a workgroup: the smallest of 16, 32 and 64 that holds all of a kv head's, or groups of 64 where none does. 64 rows are one slab with
-// D = 64, two slabs of 32 with D = 128, whose wavefronts read the same keys. Four wavefronts or eight, by the rules below. A piece starts and ends
+// D = 64, two slabs of 32 with D = 128, whose wavefronts read the same keys; or slabs of their own, by the rule above. Four wavefronts or eight, by the rules below. A piece starts and ends
 // in 8 us, pieces are joined in 5 us, and a wavefront takes 0.3 us a block when the device is full: the costs below. What is known of the lengths here
 // is max_kv_len alone.
-inline PagedPlan plan_paged(const fspad_paged_desc& d, PagedFormat = PagedFormat::kFp4) {
+inline PagedPlan plan_paged(const fspad_paged_desc& d, PagedFormat format = PagedFormat::kFp4) {
   PagedPlan pl{};
   const int rows = d.n_nodes_max * (d.n_q_heads / d.n_kv_heads);
   pl.rows_per_group = rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
   pl.groups = (rows + pl.rows_per_group - 1) / pl.rows_per_group;
   pl.rows_per_wave = pl.rows_per_group == 64 && d.head_dim == 128 ? 32 : pl.rows_per_group;
   pl.WS = pl.rows_per_group / pl.rows_per_wave;
-  const int64_t units = (int64_t)d.batch * d.n_kv_heads * pl.groups, longest = paged_unit_blocks(d);
+  const int64_t longest = paged_unit_blocks(d);
+  if (format == PagedFormat::kFp8) pl.slabs = paged_slabs(d, rows, longest);
+  if (pl.slabs) {
+    pl.rows_per_wave = rows <= 16 ? 16 : 32;
+    pl.WS = pl.waves = pl.slabs;
+    pl.rows_per_group = pl.WS * pl.rows_per_wave;
+    pl.groups = (rows + pl.rows_per_group - 1) / pl.rows_per_group;
+  }
+  const int64_t units = (int64_t)d.batch * d.n_kv_heads * pl.groups;
   // Eight wavefronts where every unit may have a compute unit to itself and they have several blocks each; else four, and workgroups that share a
   // compute unit have each other's starts and ends. One token, D = 128, 8 kv heads: 400 tokens 8.7 us on four and 9.5 on eight, 2000 13.3 and 13.2,
   // 32 sequences of 4000 32.2 and 30.7, 64 of 1000 18.2 and 21.9. 26 nodes on 32 heads: 8 sequences of 1000 15.9 and 17.5, of 2000 27.7 and 20.9, 16 of 300 .. 3000
@@ -56,7 +85,7 @@ inline PagedPlan plan_paged(const fspad_paged_desc& d, PagedFormat = PagedFormat
   // heads, 1300 16.3 and 16.0, 2048 16.8 and 18.8, 3000 21.1 and 19.6.
   const bool rows16 = pl.rows_per_wave == 16;
   const bool few = !rows16 && units <= 32 && units * longest * pl.WS <= 4400;   // as many pieces of few blocks as compute units
-  pl.waves = (pl.WS == 1 && units > kPagedComputeUnits) || longest <= (rows16 ? 48 : 36 / pl.WS) || few ? 4 : 8;
+  if (!pl.slabs) pl.waves = (pl.WS == 1 && units > kPagedComputeUnits) || longest <= (rows16 ? 48 : 36 / pl.WS) || few ? 4 : 8;
   const int key_waves = pl.waves / pl.WS;
   pl.resident = paged_resident(pl.waves, d.head_dim, rows16) * kPagedComputeUnits;
   pl.least_blocks = 2 * key_waves;
@@ -66,6 +95,9 @@ inline PagedPlan plan_paged(const fspad_paged_desc& d, PagedFormat = PagedFormat
   // 8000 53.7 and 56.1; 64 of 250 .. 4000, D = 64, 20.3 and 25.2. 26 nodes on 32 heads, eight wavefronts: 2048 19.6 and 19.4; 3000 22.8 and 19.8.
   const int cuts = (int)(kPagedComputeUnits / units);
   pl.whole_blocks = !rows16 ? 9 * key_waves : pl.waves == 4 ? 128 : cuts < 2 ? 256 : 80 * cuts / (cuts - 1);
+  // Slabs of their own: two pieces of two blocks cost more than one of four. Trees of 60 nodes on 64 heads, 8 of keys, 8 sequences of 1000 tokens, 8-bit: 41 us cut, 29 whole;
+  // 16 on 32 heads of 2000 59 and 45; 32 of 100 .. 4000 94 and 106.
+  if (pl.slabs) pl.whole_blocks = 96;
   pl.piece_cost = 8 * key_waves;
   pl.join_cost = 4 * key_waves;
   pl.dead_cost = key_waves;

@@ -119,6 +119,36 @@ def test_ragged_batches():
             assert np.all(got[b, nodes[b]:] == 0)
 
 
+@pytest.mark.parametrize("B,N,Hq,Hkv,D,P,top", [
+    (130, 1, 16, 8, 128, 32, 100), (130, 1, 16, 8, 64, 128, 300), (520, 1, 2, 2, 64, 32, 33), (100, 9, 16, 8, 128, 32, 90), (100, 9, 16, 8, 64, 64, 200),
+    (50, 20, 16, 8, 128, 64, 400), (50, 20, 16, 8, 64, 32, 400), (40, 20, 32, 8, 128, 32, 300), (40, 20, 32, 8, 64, 256, 300), (12, 60, 32, 8, 128, 32, 200)])
+def test_as_many_rows_as_the_device_has_wavefronts(B, N, Hq, Hkv, D, P, top):
+    """Wavefronts then have rows for themselves: one slab a workgroup, or four; sequences of no node, of no token, of all."""
+    rng = np.random.default_rng(B + N + D)
+    kv_len, nodes = rng.integers(0, top + 1, B), rng.integers(0, N + 1, B)
+    kv_len[:4], nodes[:4] = (0, top, 0, top), (N, N, 0, 0)
+    got = Case(B, B, N, Hq, Hkv, D, P, kv_len, nodes).check()
+    for b in range(B):
+        assert np.all(got[b, nodes[b]:] == 0)
+
+
+@pytest.mark.parametrize("workgroups", [0, 1, 9, 1000, 4096])
+@pytest.mark.parametrize("D", [128, 64])
+def test_long_ones_among_many(workgroups, D):
+    """Four slabs a workgroup, and a sequence that is cut: by itself, or as the call asks."""
+    rng = np.random.default_rng(workgroups + D)
+    kv_len, nodes = rng.integers(0, 80, 34), rng.integers(0, 21, 34)
+    kv_len[5], nodes[5], nodes[6] = 3500, 20, 0
+    Case(workgroups + D, 34, 20, 32, 8, D, 64, kv_len, nodes).check(workgroups=workgroups)
+
+
+@pytest.mark.parametrize("workgroups", [0, 1, 33, 4096])
+@pytest.mark.parametrize("N,Hq,D,L", [(33, 1, 128, 160), (60, 4, 128, 130), (60, 4, 64, 250), (64, 1, 64, 0), (60, 4, 64, 251), (33, 1, 128, 161)])
+def test_few_keys_of_a_tree(N, Hq, D, L, workgroups):
+    """Up to where a wavefront takes all keys of its rows, and one more."""
+    Case(N + D + L, 2, N, Hq, 1, D, 32, [L, L // 2], [N, N // 2]).check(workgroups=workgroups)
+
+
 def test_lengths_and_counts_outside_their_ranges_are_clamped():
     c = Case(4, 4, 6, 2, 1, 128, 32, [100, 60, 30, 5])
     c.kv_len = np.array([10 ** 6, -7, 30, 2 ** 31 - 1], np.int32)

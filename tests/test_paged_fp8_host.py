@@ -84,6 +84,20 @@ def test_attention_refuses_shapes(lib, change):
     assert lib.fspad_tree_attn_paged_byte(ctypes.byref(d), *[P16] * 9, P16, 1 << 40, None) == SHAPE
 
 
+@pytest.mark.parametrize("batch,nodes,heads,group,max_kv_len,rows,cut", [
+    (12, 60, 8, 4, 2000, 128, False), (12, 60, 8, 4, 100000, 128, True),     # 768 slabs of 32 rows: four of them a workgroup, whatever the length
+    (11, 60, 8, 4, 2000, 64, True),                                          # fewer
+    (12, 8, 32, 8, 2000, 32, False), (12, 8, 32, 8, 71 * 32, 32, False),     # rows of one slab or two: one a workgroup, up to 72 blocks
+    (12, 8, 32, 8, 71 * 32 + 1, 64, True),
+    (1, 60, 8, 4, 160, 32, False), (4, 40, 8, 1, 160, 32, False), (1, 60, 8, 4, 161, 64, False)])
+def test_attention_groups_rows(lib, batch, nodes, heads, group, max_kv_len, rows, cut):
+    """The workspace has a word pair for each unit, and slots of a unit's rows where units may be cut: it tells how rows are grouped."""
+    d = _desc(batch=batch, n_kv_heads=heads, n_q_heads=heads * group, n_nodes_max=nodes, max_kv_len=max_kv_len, page_stride=heads * PER, table_width=4096,
+              table_stride=4096)
+    need, words = fspad.fspad_tree_attn_paged_byte_workspace_bytes(d), batch * heads * -(-nodes * group // rows) * 8
+    assert (need > words) == cut and (need - words) % (rows * (128 + 2) * 4) == 0
+
+
 def test_attention_refuses_arguments(lib):
     d = _desc()
     need = fspad.fspad_tree_attn_paged_byte_workspace_bytes(d)

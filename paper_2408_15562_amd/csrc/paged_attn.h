@@ -400,7 +400,7 @@ struct Places {
 // WIDE: a page holds a block's 32 keys (pages of 16 keys: a block's halves lie on two). SPLIT: a slab has several wavefronts, which split its
 // keys; else a wavefront has a slab, and all keys of the piece, for itself.
 template <class Form, int WAVES, bool WIDE, bool SPLIT>
-__global__ __launch_bounds__(64 * WAVES, WAVES * paged_resident(WAVES, Form::HEAD_DIM, Form::ROWS == 16) / 4)
+__global__ __launch_bounds__(64 * WAVES, WAVES * paged_resident(WAVES, Form::HEAD_DIM, Form::ROWS == 16, SPLIT) / 4)
 void tree_attn_paged_kernel(const PagedParams) {
   Args p = (Args)__builtin_amdgcn_kernarg_segment_ptr();
   constexpr int D = Form::HEAD_DIM, RT = Form::RT, QUADS = Form::QUADS;

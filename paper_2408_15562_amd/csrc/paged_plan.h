@@ -15,7 +15,9 @@ constexpr int kPagedMaxBatch = 1024;
 constexpr int kPagedComputeUnits = 256;
 
 // Workgroups of a compute unit. (Three of four wavefronts, D = 128, would spill: 64 sequences of 2000 tokens, 8 kv heads, 34.2 us, two 30.6.)
-constexpr int paged_resident(int waves, int D, bool rows16) { return (rows16 && D == 64 ? 16 : 8) / waves; }
+// Slabs of their own, four of them, D = 64: three, although 31 registers go to memory: 64 trees of 60 nodes on 32 heads, 8 of keys, 500 tokens 43 -> 39 us, 2000 tokens 113 -> 100; one slab of 32 rows
+// would lose by it (256 of 7 nodes, 250 tokens 21.0 -> 22.4).
+constexpr int paged_resident(int waves, int D, bool rows16, bool split) { return (D == 128 ? 8 : rows16 ? 16 : !split && waves == 4 ? 12 : 8) / waves; }
 
 struct PagedPlan {
   int rows_per_wave, WS, waves;   // row slabs and wavefronts of a workgroup (those of a slab split its keys)
@@ -35,6 +37,8 @@ inline int64_t paged_unit_blocks(const fspad_paged_desc& d) {   // at most
   return ((int64_t)d.max_kv_len + kBlockKeys - 1) / kBlockKeys + (d.n_nodes_max + kBlockKeys - 1) / kBlockKeys;
 }
 
+constexpr int kSlabWhole = 96;   // units of so many blocks are never cut where slabs have wavefronts of their own
+
 // Whether wavefronts of a call over the 8-bit cache have rows for themselves, with all their keys: a wavefront then starts once for its rows, and nothing
 // is merged. Where there are enough such slabs for the device that is what it costs to start that counts, not how long one takes. 0: they do not; else slabs a workgroup, one,
 // or four where a kv head has more than 64 rows (they read the same keys). Split by four or eight wavefronts / slabs of their own, us; heads are query heads on kv heads:
@@ -43,14 +47,14 @@ inline int64_t paged_unit_blocks(const fspad_paged_desc& d) {   // at most
 //   7 nodes, 32 on 8, D = 128: 64 (512) of 50 .. 1000 22 / 25, 96 (768) 36 / 35, of 2000 94 / 79, 256 of 500 81 / 64; 192 of 50 .. 4000 186 / 200. D = 64: 64 of 50 .. 1000 14.8 / 19.4, 96
 //     21.4 / 20.4, 256 of 500 53 / 36.
 //   60 nodes, 16 on 16, D = 128: 16 (512) of 1000 22 / 27, 24 (768) 44 / 36, 64 of 500 53 / 47, 64 of 1000 .. 8000 309 / 487.
-//   60 nodes, 32 on 8, D = 128: 8 (512) of 500 17.4 / 20.6, 12 (768) 24 / 21.5, of 2000 59 / 41, of 50 .. 4000 70 / 64, 64 of 500 91 / 70, of 2000 249 / 168. D = 64: 12 of 2000 35 / 31, 64 of 500
-//     70 / 41; four slabs a workgroup 70, one 74 (64 of 500, D = 128), and of 50 .. 4000 222 and 366.
+//   60 nodes, 32 on 8, D = 128: 8 (512) of 500 17.4 / 20.6, 12 (768) 24 / 21.5, of 2000 59 / 41, of 50 .. 4000 70 / 64, 64 of 500 91 / 70, of 2000 249 / 168. D = 64: 12 of 2000 35 / 31, of 8000
+//     80 / 83, 16 (1024) of 50 .. 4000 47 / 51, 32 (2048) 83 / 74, 64 of 500 70 / 40; four slabs a workgroup 70, one 74 (64 of 500, D = 128), and of 50 .. 4000 222 and 366.
 // More than 32 rows and few keys: the merge takes longer than the keys of one wavefront. One sequence, 60 nodes, 32 on 8, D = 128: one token 11.4 / 10.2, 100 12.1 / 11.7, 250 13.2 / 13.2;
 // 36 nodes on 40 heads, 4 sequences of 100 12.8 / 13.3, of 250 14.0 / 15.2; D = 64, 60 nodes: 1 9.4 / 8.6, 250 12.0 / 11.0, 500 13.5 / 13.5. 7 nodes: 30 tokens 8.6 / 9.1.
 inline int paged_slabs(const fspad_paged_desc& d, int rows, int64_t longest) {
   const int per_wave = rows <= 16 ? 16 : 32;
   const int64_t slabs = (int64_t)d.batch * d.n_kv_heads * ((rows + per_wave - 1) / per_wave);
-  const bool many = slabs >= (rows <= 16 ? 4 : 3) * kPagedComputeUnits;
+  const bool many = slabs >= (rows <= 16 ? 4 : d.head_dim == 64 && longest > kSlabWhole ? 6 : 3) * kPagedComputeUnits;
   if (many && rows > 64) return 4;
   return (many && longest <= 72) || (rows > 32 && longest <= (d.head_dim == 64 ? 10 : 7)) ? 1 : 0;
 }
@@ -87,7 +91,7 @@ inline PagedPlan plan_paged(const fspad_paged_desc& d, PagedFormat format = Page
   const bool few = !rows16 && units <= 32 && units * longest * pl.WS <= 4400;   // as many pieces of few blocks as compute units
   if (!pl.slabs) pl.waves = (pl.WS == 1 && units > kPagedComputeUnits) || longest <= (rows16 ? 48 : 36 / pl.WS) || few ? 4 : 8;
   const int key_waves = pl.waves / pl.WS;
-  pl.resident = paged_resident(pl.waves, d.head_dim, rows16) * kPagedComputeUnits;
+  pl.resident = paged_resident(pl.waves, d.head_dim, rows16, pl.slabs == 0) * kPagedComputeUnits;
   pl.least_blocks = 2 * key_waves;
   // Joining costs as much as 80 blocks of 16 rows take eight wavefronts, 9 blocks a wavefront of 32 rows; cutting saves nothing where there are as
   // many units as workgroups, and half of a unit where there are half as many. One token, D = 128, 8 kv heads, whole and cut: 1 sequence of
@@ -97,7 +101,7 @@ inline PagedPlan plan_paged(const fspad_paged_desc& d, PagedFormat format = Page
   pl.whole_blocks = !rows16 ? 9 * key_waves : pl.waves == 4 ? 128 : cuts < 2 ? 256 : 80 * cuts / (cuts - 1);
   // Slabs of their own: two pieces of two blocks cost more than one of four. Trees of 60 nodes on 64 heads, 8 of keys, 8 sequences of 1000 tokens, 8-bit: 41 us cut, 29 whole;
   // 16 on 32 heads of 2000 59 and 45; 32 of 100 .. 4000 94 and 106.
-  if (pl.slabs) pl.whole_blocks = 96;
+  if (pl.slabs) pl.whole_blocks = kSlabWhole;
   pl.piece_cost = 8 * key_waves;
   pl.join_cost = 4 * key_waves;
   pl.dead_cost = key_waves;

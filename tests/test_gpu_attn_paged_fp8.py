@@ -136,10 +136,10 @@ def test_as_many_rows_as_the_device_has_wavefronts(B, N, Hq, Hkv, D, P, top):
 @pytest.mark.parametrize("D", [128, 64])
 def test_long_ones_among_many(workgroups, D):
     """Four slabs a workgroup, and a sequence that is cut: by itself, or as the call asks."""
-    rng = np.random.default_rng(workgroups + D)
-    kv_len, nodes = rng.integers(0, 80, 34), rng.integers(0, 21, 34)
+    rng, B = np.random.default_rng(workgroups + D), 34 if D == 128 else 66
+    kv_len, nodes = rng.integers(0, 80, B), rng.integers(0, 21, B)
     kv_len[5], nodes[5], nodes[6] = 3500, 20, 0
-    Case(workgroups + D, 34, 20, 32, 8, D, 64, kv_len, nodes).check(workgroups=workgroups)
+    Case(workgroups + D, B, 20, 32, 8, D, 64, kv_len, nodes).check(workgroups=workgroups)
 
 
 @pytest.mark.parametrize("workgroups", [0, 1, 33, 4096])

@@ -91,11 +91,22 @@ def test_attention_refuses_shapes(lib, change):
     (12, 8, 32, 8, 71 * 32 + 1, 64, True),
     (1, 60, 8, 4, 160, 32, False), (4, 40, 8, 1, 160, 32, False), (1, 60, 8, 4, 161, 64, False)])
 def test_attention_groups_rows(lib, batch, nodes, heads, group, max_kv_len, rows, cut):
+    _groups_rows(128, batch, nodes, heads, group, max_kv_len, rows, cut)
+
+
+@pytest.mark.parametrize("batch,nodes,heads,group,max_kv_len,rows,cut", [
+    (12, 60, 8, 4, 94 * 32, 128, False), (12, 60, 8, 4, 94 * 32 + 1, 64, True), (24, 60, 8, 4, 94 * 32 + 1, 128, True), (1, 60, 8, 4, 256, 32, False),
+    (1, 60, 8, 4, 257, 64, False)])
+def test_attention_groups_rows_of_64_channels(lib, batch, nodes, heads, group, max_kv_len, rows, cut):
+    _groups_rows(64, batch, nodes, heads, group, max_kv_len, rows, cut)
+
+
+def _groups_rows(D, batch, nodes, heads, group, max_kv_len, rows, cut):
     """The workspace has a word pair for each unit, and slots of a unit's rows where units may be cut: it tells how rows are grouped."""
-    d = _desc(batch=batch, n_kv_heads=heads, n_q_heads=heads * group, n_nodes_max=nodes, max_kv_len=max_kv_len, page_stride=heads * PER, table_width=4096,
-              table_stride=4096)
+    d = _desc(batch=batch, n_kv_heads=heads, n_q_heads=heads * group, n_nodes_max=nodes, max_kv_len=max_kv_len, head_dim=D, page_stride=heads * (2 * 32 * D + 16),
+              table_width=4096, table_stride=4096)
     need, words = fspad.fspad_tree_attn_paged_byte_workspace_bytes(d), batch * heads * -(-nodes * group // rows) * 8
-    assert (need > words) == cut and (need - words) % (rows * (128 + 2) * 4) == 0
+    assert (need > words) == cut and (need - words) % (rows * (D + 2) * 4) == 0
 
 
 def test_attention_refuses_arguments(lib):

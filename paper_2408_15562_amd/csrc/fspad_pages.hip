@@ -48,7 +48,7 @@ __device__ __forceinline__ int sum_before(int x, int* wave_sum, int& all) {
   return before + s - x;
 }
 
-// Calls fn(i, entry) for the first n entries of a row, from sixteen lanes of which this is one.
+// Calls fn(i, entry) for the first n entries of a row, from sixteen lanes of which this is one, and with an entry of -1 for some i behind them.
 template <typename Fn>
 __device__ __forceinline__ void along_row(const int32_t* row, int n, Fn&& fn) {
   for (int i0 = threadIdx.x % kRowLanes; i0 < n; i0 += kRowLanes * kInFlight) {
@@ -56,13 +56,14 @@ __device__ __forceinline__ void along_row(const int32_t* row, int n, Fn&& fn) {
 #pragma unroll
     for (int k = 0; k < kInFlight; ++k) e[k] = i0 + k * kRowLanes < n ? row[i0 + k * kRowLanes] : -1;
 #pragma unroll
-    for (int k = 0; k < kInFlight; ++k)
-      if (i0 + k * kRowLanes < n) fn(i0 + k * kRowLanes, e[k]);
+    for (int k = 0; k < kInFlight; ++k) fn(i0 + k * kRowLanes, e[k]);
   }
 }
 
 // How `shared` changes: a workgroup counts in LDS what happens to its own pages, for which it looks through all entries that the call is about. No
-// atomics on memory: 70000 of them took 50 us (1024 rows of 31 to 250 pages, half of them released), the look takes 14, and 3.5 in a call of a few rows.
+// atomics on memory: 70000 of them took 50 us (1024 rows of 31 to 250 pages, half of them released), the look takes 13, and 3.5 in a call of a few rows. What bounds it is what a compute unit
+// gets from the caches, 31 bytes a ns (35 KB of entries 1.1 us; more requests out, workgroups that fetch ahead for the die, entries four at a time: the same). Eight workgroups a tile and a launch that joins them
+// take 13 us for 18 there, but 12 for 9 where few of many sequences end.
 
 // ---------------------------------------------------------------------------------------------
 // Fork.
@@ -164,6 +165,7 @@ __global__ __launch_bounds__(kThreads) void page_fork_kernel(const ForkParams p)
     if (n_full == 0 || !(own || page0 < page1)) continue;
     int32_t* const to = p.table + to_row[f] * p.table_stride;
     along_row(p.table + from_row[f] * p.table_stride, n_full, [&](int i, int page) {
+      if (i >= n_full) return;
       if (own) to[i] = page;
       if (page >= page0 && page < page1) atomicAdd(&counts[page - page0], 1);
     });
@@ -216,7 +218,8 @@ __global__ __launch_bounds__(kThreads) void page_release_kernel(const ReleasePar
   __syncthreads();
   for (int r = tid / kRowLanes; r < n_rows; r += kRowsAtOnce)
     along_row(p.table + row[r] * p.table_stride, held[r], [&](int, int page) {
-      if (page >= page0 && page < page1) atomicAdd(&counts[page - page0], 1);
+      const unsigned x = (unsigned)page - page0;
+      if (x < (unsigned)(page1 - page0)) atomicAdd(&counts[x], 1);
     });
   __syncthreads();
   int height = n_free;

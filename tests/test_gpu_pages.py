@@ -110,7 +110,7 @@ def test_no_forks(B, n_pages, width):
     assert got[0].numel() == 0 and torch.equal(table, before) and torch.equal(got[2], lens) and torch.equal(got[3], n_free) and torch.equal(got[4], shared)
 
 
-@pytest.mark.parametrize("B,P,n_pages,width", SIZES)
+@pytest.mark.parametrize("B,P,n_pages,width", SIZES + [(3, 16, 20000, 6000), (70, 16, 66000, 700), (9, 16, 1 << 19, 4), (300, 16, 1 << 19, 300)])
 @pytest.mark.parametrize("place", ["apart", "in place", "bad entries"])
 @pytest.mark.parametrize("part", [0.0, 0.4, 1.0])
 def test_release(B, P, n_pages, width, place, part):

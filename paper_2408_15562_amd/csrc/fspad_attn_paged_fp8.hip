@@ -27,14 +27,17 @@ namespace {
 
 template <int D>
 void launch_rows(const PagedPlan& pl, const PagedParams& p, hipStream_t stream) {
-  if (pl.slabs) {
-    if (pl.rows_per_wave == 16) launch<Form16Fp8<D>, 1, true, false>(pl, p, stream);
-    else pl.slabs == 1 ? launch<Form32Fp8<D, 1>, 1, true, false>(pl, p, stream) : launch<Form32Fp8<D, 1>, 4, true, false>(pl, p, stream);
-    return;
+  if (pl.rows_per_wave == 16) {
+    if (!pl.split) launch<Form16Fp8<D>, 1, true, false>(pl, p, stream);
+    else if (pl.waves == 2) launch<Form16Fp8<D>, 2, true>(pl, p, stream);
+    else pl.waves == 4 ? launch<Form16Fp8<D>, 4, true>(pl, p, stream) : launch<Form16Fp8<D>, 8, true>(pl, p, stream);
+  } else if (pl.rows_per_wave == 32) {
+    if (!pl.split) pl.WS == 1 ? launch<Form32Fp8<D, 1>, 1, true, false>(pl, p, stream) : launch<Form32Fp8<D, 1>, 4, true, false>(pl, p, stream);
+    else if (pl.waves == 2) launch<Form32Fp8<D, 1>, 2, true>(pl, p, stream);
+    else pl.waves == 4 ? launch<Form32Fp8<D, 1>, 4, true>(pl, p, stream) : launch<Form32Fp8<D, 1>, 8, true>(pl, p, stream);
+  } else if constexpr (D == 64) {
+    pl.waves == 4 ? launch<Form32Fp8<64, 2>, 4, true>(pl, p, stream) : launch<Form32Fp8<64, 2>, 8, true>(pl, p, stream);
   }
-  if (pl.rows_per_wave == 16) pl.waves == 4 ? launch<Form16Fp8<D>, 4, true>(pl, p, stream) : launch<Form16Fp8<D>, 8, true>(pl, p, stream);
-  else if (pl.rows_per_wave == 32) pl.waves == 4 ? launch<Form32Fp8<D, 1>, 4, true>(pl, p, stream) : launch<Form32Fp8<D, 1>, 8, true>(pl, p, stream);
-  else if constexpr (D == 64) pl.waves == 4 ? launch<Form32Fp8<64, 2>, 4, true>(pl, p, stream) : launch<Form32Fp8<64, 2>, 8, true>(pl, p, stream);
 }
 
 }  // namespace

@@ -19,6 +19,8 @@ constexpr int kPagedComputeUnits = 256;
 // would lose by it (256 of 7 nodes, 250 tokens 21.0 -> 22.4).
 constexpr int paged_resident(int waves, int D, bool rows16, bool split) { return (D == 128 ? 8 : rows16 ? 16 : !split && waves == 4 ? 12 : 8) / waves; }
 
+constexpr int kSlabWhole = 96;   // units of so many blocks are not cut where a slab has four wavefronts or fewer, 8-bit
+
 struct PagedPlan {
   int rows_per_wave, WS, waves;   // row slabs and wavefronts of a workgroup (those of a slab split its keys)
   int rows_per_group;    // WS * rows_per_wave: 16, 32 or 64
@@ -26,7 +28,7 @@ struct PagedPlan {
   int resident;          // workgroups that the device holds at once
   int least_blocks, whole_blocks;   // no piece is shorter, no unit of up to so many blocks is cut
   int piece_cost, join_cost, dead_cost;   // what starting and ending a piece takes, joining pieces, a unit without nodes, in blocks
-  int slabs;             // slabs of a workgroup if a wavefront has all keys of its rows; 0: those of a slab split its keys
+  bool split;            // a slab's wavefronts split its keys, else there is one
   bool may_cut;          // a unit can be so long that it is cut
   bool lines;            // workgroups may take windows of all units: two slots each
   int max_pieces;
@@ -37,30 +39,39 @@ inline int64_t paged_unit_blocks(const fspad_paged_desc& d) {   // at most
   return ((int64_t)d.max_kv_len + kBlockKeys - 1) / kBlockKeys + (d.n_nodes_max + kBlockKeys - 1) / kBlockKeys;
 }
 
-constexpr int kSlabWhole = 96;   // units of so many blocks are never cut where slabs have wavefronts of their own
-
-// Whether wavefronts of a call over the 8-bit cache have rows for themselves, with all their keys: a wavefront then starts once for its rows, and nothing
-// is merged. Where there are enough such slabs for the device that is what it costs to start that counts, not how long one takes. 0: they do not; else slabs a workgroup, one,
-// or four where a kv head has more than 64 rows (they read the same keys). Split by four or eight wavefronts / slabs of their own, us; heads are query heads on kv heads:
-//   one token, 32 on 8, D = 128: 64 sequences (512 slabs) of 250 tokens 12.0 / 12.5, 96 of 50 .. 2000 54.5 / 55.6; 128 (1024) of 100 19.2 / 13.1, of 1000 59 / 56, of 50 .. 2000
-//     69 / 70, of 4000 182 / 193; 256 of 100 36 / 19, of 1000 104 / 100. D = 64: 96 of 50 .. 1000 15.3 / 17.7, 256 of 250 24.4 / 17.6, of 50 .. 1000 44 / 38.
-//   7 nodes, 32 on 8, D = 128: 64 (512) of 50 .. 1000 22 / 25, 96 (768) 36 / 35, of 2000 94 / 79, 256 of 500 81 / 64; 192 of 50 .. 4000 186 / 200. D = 64: 64 of 50 .. 1000 14.8 / 19.4, 96
-//     21.4 / 20.4, 256 of 500 53 / 36.
-//   60 nodes, 16 on 16, D = 128: 16 (512) of 1000 22 / 27, 24 (768) 44 / 36, 64 of 500 53 / 47, 64 of 1000 .. 8000 309 / 487.
-//   60 nodes, 32 on 8, D = 128: 8 (512) of 500 17.4 / 20.6, 12 (768) 24 / 21.5, of 2000 59 / 41, of 50 .. 4000 70 / 64, 64 of 500 91 / 70, of 2000 249 / 168. D = 64: 12 of 2000 35 / 31, of 8000
-//     80 / 83, 16 (1024) of 50 .. 4000 47 / 51, 32 (2048) 83 / 74, 64 of 500 70 / 40; four slabs a workgroup 70, one 74 (64 of 500, D = 128), and of 50 .. 4000 222 and 366.
-// More than 32 rows and few keys: the merge takes longer than the keys of one wavefront. One sequence, 60 nodes, 32 on 8, D = 128: one token 11.4 / 10.2, 100 12.1 / 11.7, 250 13.2 / 13.2;
-// 36 nodes on 40 heads, 4 sequences of 100 12.8 / 13.3, of 250 14.0 / 15.2; D = 64, 60 nodes: 1 9.4 / 8.6, 250 12.0 / 11.0, 500 13.5 / 13.5. 7 nodes: 30 tokens 8.6 / 9.1.
-inline int paged_slabs(const fspad_paged_desc& d, int rows, int64_t longest) {
+// How a call over the 8-bit cache deals its rows out: in slabs of 16 or 32 rows (WS of them a workgroup), and a slab's keys to `key_waves` wavefronts. Two slabs, or one of 64 rows,
+// in a workgroup read keys once for both, but a workgroup of one slab is lighter, and a wavefront that has all keys of its rows merges nothing. Chosen / otherwise, us; query heads on kv heads:
+// Fewer slabs than compute units: one a workgroup, four wavefronts up to 72 blocks, then eight, if the pieces fill three quarters of the device. 60 nodes, 16 on 16, D = 128, in groups of 64 rows: 4 sequences of 300
+//   tokens 11.2 / 14.0, 1000 15.0 / 19.7, 2000 18.4 / 23.9, on eight wavefronts 19.1; 32 on 8: 4 of 1000 15.7 / 20.3, 2000 19.8 / 29.4, 4000 26 / 33, on four 32; 64 on 8, 16384 44 / 46. D = 64: 4 of 1000 11.7 / 16.3,
+//   4000 18 / 23. 160 rows of 32 heads, 9946 tokens: 48 / 57 in slabs.
+// More: the same on four wavefronts up to 72 blocks; D = 128 from 37 on. 4 of 60 nodes, 64 on 8: 500 tokens 17.4 / 18.4 in slabs, 2000 28 / 31; D = 64: 500 13.1 / 14.6, 2000 21 / 24; 4 of 36 on 40, 8000 49 / 64 in slabs.
+// Three a compute unit (16 rows: four; long ones, D = 64: six) and more than 64 rows: four a workgroup, a wavefront each. 60 nodes, 32 on 8, D = 128: 8 sequences (512 slabs) of 500 17.4 / 20.6 so, 12 (768)
+//   21.5 / 24, of 2000 41 / 59, of 50 .. 4000 64 / 70, 64 of 500 70 / 91, of 2000 168 / 249. D = 64: 12 of 2000 31 / 35, of 8000 80 / 83 so, 64 of 500 40 / 70.
+// The same, 64 rows or fewer, up to 72 blocks: a workgroup is a slab, of one wavefront where they are short or six a compute unit, else of two. One token, 32 on 8, D = 128: 64 sequences (512 slabs) of 250
+//   12.0 / 12.5 so, 128 (1024) of 30 9.3 / 13.8, of 500 30 / 36 on four and on one, of 50 .. 2000 62 / 69 and 69, of 4000 182 / 193 so; 256 of 100 19 / 36 on four, of 1000 100 / 104. D = 64: 128 of 50 .. 2000 35 / 39 and 43. 7 nodes,
+//   D = 128: 64 of 50 .. 1000 22 / 25 so, 96 (768) of 500 27 / 31 and 30, 256 of 500 64 / 81; D = 64: 96 of 50 .. 2000 32 / 40 and 41. 60 nodes, 16 on 16: 32 (1024) of 1000 39 / 45 and 44, of 1000 .. 8000 172 / 228 so.
+// More than 32 rows and few keys: one wavefront a slab. 60 nodes, 32 on 8, D = 128: one token 10.2 / 11.4, 250 13.2 / 13.2; D = 64: 8.6 / 9.4, 250 11.0 / 12.0, 500 13.5 / 13.5.
+struct PagedRows {
+  int per_wave, WS, key_waves;   // key_waves 0: as over the 4-bit cache
+};
+inline PagedRows paged_rows_fp8(const fspad_paged_desc& d, int rows, int64_t longest) {
   const int per_wave = rows <= 16 ? 16 : 32;
   const int64_t slabs = (int64_t)d.batch * d.n_kv_heads * ((rows + per_wave - 1) / per_wave);
   const bool many = slabs >= (rows <= 16 ? 4 : d.head_dim == 64 && longest > kSlabWhole ? 6 : 3) * kPagedComputeUnits;
-  if (many && rows > 64) return 4;
-  return (many && longest <= 72) || (rows > 32 && longest <= (d.head_dim == 64 ? 10 : 7)) ? 1 : 0;
+  if (many && rows > 64) return {per_wave, 4, 1};
+  if (rows > 32 && longest <= (d.head_dim == 64 ? 10 : 7)) return {per_wave, 1, 1};
+  if (many && longest <= 72) return {per_wave, 1, longest <= (rows <= 16 ? 8 : 12) || slabs >= 6 * kPagedComputeUnits ? 1 : 2};
+  if (rows <= 16) return {16, 1, 0};
+  if (slabs <= kPagedComputeUnits) {
+    if (longest <= 72) return {32, 1, 4};
+    if (rows <= 32 || kPagedComputeUnits / slabs * slabs >= 192) return {32, 1, 8};
+  }
+  if (rows <= 32 || (longest <= 72 && (d.head_dim == 64 || longest > 36))) return {32, 1, 4};
+  return {32, 1, 0};
 }
 
 // Rows of a workgroup: the smallest of 16, 32 and 64 that holds all of a kv head's, or groups of 64 where none does. 64 rows are one slab with
-// D = 64, two slabs of 32 with D = 128, whose wavefronts read the same keys; or slabs of their own, by the rule above. Four wavefronts or eight, by the rules below. A piece starts and ends
+// D = 64, two slabs of 32 with D = 128, whose wavefronts read the same keys; over the 8-bit cache by the rule above, where it gives one. Four wavefronts or eight, by the rules below. A piece starts and ends
 // in 8 us, pieces are joined in 5 us, and a wavefront takes 0.3 us a block when the device is full: the costs below. What is known of the lengths here
 // is max_kv_len alone.
 inline PagedPlan plan_paged(const fspad_paged_desc& d, PagedFormat format = PagedFormat::kFp4) {
@@ -71,13 +82,14 @@ inline PagedPlan plan_paged(const fspad_paged_desc& d, PagedFormat format = Page
   pl.rows_per_wave = pl.rows_per_group == 64 && d.head_dim == 128 ? 32 : pl.rows_per_group;
   pl.WS = pl.rows_per_group / pl.rows_per_wave;
   const int64_t longest = paged_unit_blocks(d);
-  if (format == PagedFormat::kFp8) pl.slabs = paged_slabs(d, rows, longest);
-  if (pl.slabs) {
-    pl.rows_per_wave = rows <= 16 ? 16 : 32;
-    pl.WS = pl.waves = pl.slabs;
+  const PagedRows dealt = format == PagedFormat::kFp8 ? paged_rows_fp8(d, rows, longest) : PagedRows{};
+  if (dealt.key_waves) {
+    pl.rows_per_wave = dealt.per_wave;
+    pl.WS = dealt.WS;
     pl.rows_per_group = pl.WS * pl.rows_per_wave;
     pl.groups = (rows + pl.rows_per_group - 1) / pl.rows_per_group;
   }
+  pl.split = dealt.key_waves != 1;
   const int64_t units = (int64_t)d.batch * d.n_kv_heads * pl.groups;
   // Eight wavefronts where every unit may have a compute unit to itself and they have several blocks each; else four, and workgroups that share a
   // compute unit have each other's starts and ends. One token, D = 128, 8 kv heads: 400 tokens 8.7 us on four and 9.5 on eight, 2000 13.3 and 13.2,
@@ -89,9 +101,9 @@ inline PagedPlan plan_paged(const fspad_paged_desc& d, PagedFormat format = Page
   // heads, 1300 16.3 and 16.0, 2048 16.8 and 18.8, 3000 21.1 and 19.6.
   const bool rows16 = pl.rows_per_wave == 16;
   const bool few = !rows16 && units <= 32 && units * longest * pl.WS <= 4400;   // as many pieces of few blocks as compute units
-  if (!pl.slabs) pl.waves = (pl.WS == 1 && units > kPagedComputeUnits) || longest <= (rows16 ? 48 : 36 / pl.WS) || few ? 4 : 8;
+  pl.waves = dealt.key_waves ? dealt.key_waves * pl.WS : (pl.WS == 1 && units > kPagedComputeUnits) || longest <= (rows16 ? 48 : 36 / pl.WS) || few ? 4 : 8;
   const int key_waves = pl.waves / pl.WS;
-  pl.resident = paged_resident(pl.waves, d.head_dim, rows16, pl.slabs == 0) * kPagedComputeUnits;
+  pl.resident = paged_resident(pl.waves, d.head_dim, rows16, pl.split) * kPagedComputeUnits;
   pl.least_blocks = 2 * key_waves;
   // Joining costs as much as 80 blocks of 16 rows take eight wavefronts, 9 blocks a wavefront of 32 rows; cutting saves nothing where there are as
   // many units as workgroups, and half of a unit where there are half as many. One token, D = 128, 8 kv heads, whole and cut: 1 sequence of
@@ -99,9 +111,8 @@ inline PagedPlan plan_paged(const fspad_paged_desc& d, PagedFormat format = Page
   // 8000 53.7 and 56.1; 64 of 250 .. 4000, D = 64, 20.3 and 25.2. 26 nodes on 32 heads, eight wavefronts: 2048 19.6 and 19.4; 3000 22.8 and 19.8.
   const int cuts = (int)(kPagedComputeUnits / units);
   pl.whole_blocks = !rows16 ? 9 * key_waves : pl.waves == 4 ? 128 : cuts < 2 ? 256 : 80 * cuts / (cuts - 1);
-  // Slabs of their own: two pieces of two blocks cost more than one of four. Trees of 60 nodes on 64 heads, 8 of keys, 8 sequences of 1000 tokens, 8-bit: 41 us cut, 29 whole;
-  // 16 on 32 heads of 2000 59 and 45; 32 of 100 .. 4000 94 and 106.
-  if (pl.slabs) pl.whole_blocks = kSlabWhole;
+  // 8-bit: 8 sequences of 1000 tokens, 60 nodes on 64 heads, 8 of keys, on one wavefront 41 us cut, 29 whole; 16 on 32 heads of 2000 59 and 45; 32 of 100 .. 4000 94 and 106. On four, 4 of 2000 on 32 heads 29 and 20.
+  if (dealt.key_waves) pl.whole_blocks = key_waves <= 4 ? kSlabWhole : cuts < 2 ? 256 : 80 * cuts / (cuts - 1);
   pl.piece_cost = 8 * key_waves;
   pl.join_cost = 4 * key_waves;
   pl.dead_cost = key_waves;

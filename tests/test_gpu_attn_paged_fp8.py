@@ -132,6 +132,16 @@ def test_as_many_rows_as_the_device_has_wavefronts(B, N, Hq, Hkv, D, P, top):
         assert np.all(got[b, nodes[b]:] == 0)
 
 
+@pytest.mark.parametrize("B,N,Hq,Hkv,D,top", [
+    (130, 1, 8, 8, 128, 400), (130, 2, 8, 8, 64, 700), (100, 9, 16, 8, 128, 600), (50, 20, 16, 8, 64, 600), (2, 60, 4, 1, 128, 700), (3, 60, 4, 1, 64, 900), (1, 60, 4, 2, 128, 3000),
+    (2, 26, 4, 4, 64, 2600), (11, 60, 16, 8, 64, 500), (11, 60, 16, 8, 128, 1300)])
+def test_keys_of_a_slab_between_two_wavefronts_four_and_eight(B, N, Hq, Hkv, D, top):
+    rng = np.random.default_rng(B + N + D + top)
+    kv_len, nodes = rng.integers(0, top + 1, B) // (1 + rng.integers(0, 8, B)), rng.integers(0, N + 1, B)
+    kv_len[0], nodes[0] = top, N
+    Case(B + top, B, N, Hq, Hkv, D, 32, kv_len, nodes).check()
+
+
 @pytest.mark.parametrize("workgroups", [0, 1, 9, 1000, 4096])
 @pytest.mark.parametrize("D", [128, 64])
 def test_long_ones_among_many(workgroups, D):

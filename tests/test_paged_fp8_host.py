@@ -86,17 +86,18 @@ def test_attention_refuses_shapes(lib, change):
 
 @pytest.mark.parametrize("batch,nodes,heads,group,max_kv_len,rows,cut", [
     (12, 60, 8, 4, 2000, 128, False), (12, 60, 8, 4, 100000, 128, True),     # 768 slabs of 32 rows: four of them a workgroup, whatever the length
-    (11, 60, 8, 4, 2000, 64, True),                                          # fewer
+    (11, 60, 8, 4, 2000, 32, False), (11, 60, 8, 4, 34 * 32, 64, False), (11, 60, 8, 4, 70 * 32 + 1, 64, True),   # fewer
     (12, 8, 32, 8, 2000, 32, False), (12, 8, 32, 8, 71 * 32, 32, False),     # rows of one slab or two: one a workgroup, up to 72 blocks
     (12, 8, 32, 8, 71 * 32 + 1, 64, True),
-    (1, 60, 8, 4, 160, 32, False), (4, 40, 8, 1, 160, 32, False), (1, 60, 8, 4, 161, 64, False)])
+    (4, 60, 8, 4, 70 * 32, 32, False), (4, 60, 8, 4, 254 * 32, 32, False), (4, 60, 8, 4, 254 * 32 + 1, 32, True), (5, 60, 8, 4, 100000, 64, True), (1, 20, 32, 8, 9946, 64, True),
+    (1, 60, 8, 4, 160, 32, False), (4, 40, 8, 1, 160, 32, False)])
 def test_attention_groups_rows(lib, batch, nodes, heads, group, max_kv_len, rows, cut):
     _groups_rows(128, batch, nodes, heads, group, max_kv_len, rows, cut)
 
 
 @pytest.mark.parametrize("batch,nodes,heads,group,max_kv_len,rows,cut", [
-    (12, 60, 8, 4, 94 * 32, 128, False), (12, 60, 8, 4, 94 * 32 + 1, 64, True), (24, 60, 8, 4, 94 * 32 + 1, 128, True), (1, 60, 8, 4, 256, 32, False),
-    (1, 60, 8, 4, 257, 64, False)])
+    (12, 60, 8, 4, 94 * 32, 128, False), (12, 60, 8, 4, 94 * 32 + 1, 64, True), (24, 60, 8, 4, 94 * 32 + 1, 128, True), (11, 60, 8, 4, 34 * 32, 32, False),
+    (1, 60, 8, 4, 256, 32, False), (1, 60, 8, 4, 257, 32, False)])
 def test_attention_groups_rows_of_64_channels(lib, batch, nodes, heads, group, max_kv_len, rows, cut):
     _groups_rows(64, batch, nodes, heads, group, max_kv_len, rows, cut)
 

@@ -5,13 +5,13 @@
 // (540 clocks), against 155 and 16 of the 4-bit cache: the pages hold V's codes key after key, so that nothing is turned.
 //
 // What bounds it. Single tokens: memory. 64 sequences of 4000 tokens, 8 kv heads of D = 64 (262 MB), 49 us; 32 of them, D = 128, 50 us, 16384 tokens 188 us: 5.3 to 5.7 TB/s, 5.9 for
-// longer ones. Trees on grouped heads: products and vector instructions, which do not hide each other here (64 on 8 kv heads, 60 nodes, 16384 tokens: 45 us, 730 TFLOP/s; 28 more for 16384 more,
-// 1140 TFLOP/s; the same without any loads). The matrix cores are busy for 44 % of a SIMD's clocks, the vector unit for 62. Trees on heads of their own: both (4 sequences of 4096 tokens, 60 nodes and 52 heads,
+// longer ones. Trees on grouped heads: products and vector instructions, which do not hide each other here (64 on 8 kv heads, 60 nodes, 16384 tokens: 44 us, 750 TFLOP/s; 30 more for 16384 more,
+// 1060 TFLOP/s; the same without any loads). The matrix cores are busy for 44 % of a SIMD's clocks, the vector unit for 62. Trees on heads of their own: both (4 sequences of 4096 tokens, 60 nodes and 52 heads,
 // 231 MB: 59 us, 45 without loads). Of each, 6 (a token) to 11 us (trees) are starts, merges and joins.
 // Tried at the last two, and not kept: exponentials and conversions between the products by scheduling groups, eight ways (60.3 to 61.0 for 60.9 us and 45.3 to 47.6 for 46.6);
 // loads two turns ahead (16 rows, one token 8.8 -> 9.3 us, 32 tokens of 4000 51.1 -> 49.9; 32 rows of D = 128 spill); loads past the caches (59 -> 69 and 46 -> 58).
-// Many sequences: wavefronts with rows for themselves (256 single tokens of 100 tokens, 32 on 8 heads 36 -> 19 us; 64 trees of 60 nodes, 500 tokens, D = 64 70 -> 41; of 2000, D = 128 249 -> 168), by the
-// rule at paged_slabs.
+// How rows and keys are dealt out to wavefronts is a rule with measurements of its own, at paged_rows_fp8: 256 single tokens of 100 tokens, 32 on 8 heads 19 us and not 36; 64 trees of 60 nodes, 2000 tokens 168
+// and not 249; 4 of 1000 tokens 15.7 and not 20.3.
 // Units go head by head: every die then has some heads of all sequences instead of all heads of some, whose lengths differ (16 ragged trees 73.0 -> 69.6 us).
 #include <hip/hip_runtime.h>
 #include <stddef.h>

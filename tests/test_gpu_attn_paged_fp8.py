@@ -139,7 +139,9 @@ def test_keys_of_a_slab_between_two_wavefronts_four_and_eight(B, N, Hq, Hkv, D, 
     rng = np.random.default_rng(B + N + D + top)
     kv_len, nodes = rng.integers(0, top + 1, B) // (1 + rng.integers(0, 8, B)), rng.integers(0, N + 1, B)
     kv_len[0], nodes[0] = top, N
-    Case(B + top, B, N, Hq, Hkv, D, 32, kv_len, nodes).check()
+    case = Case(B + top, B, N, Hq, Hkv, D, 32, kv_len, nodes)
+    case.check()
+    case.check(workgroups=1500)
 
 
 @pytest.mark.parametrize("workgroups", [0, 1, 9, 1000, 4096])

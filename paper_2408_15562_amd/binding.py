@@ -234,6 +234,24 @@ def _stream_ptr(stream) -> int:
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
+def _empty(stream, shape, dtype, device) -> torch.Tensor:
+    """Memory that a call takes for itself: a workspace or an output that was not given. It is taken on the stream that the call goes to. Taken on the current
+    one, as torch.empty does, it could be memory whose last user still runs there, and a workspace, which goes back when the call has been issued, could be given
+    to that stream's next allocation while the kernels still use it. Outputs are read on the current stream as a rule: what they held is not given away before that
+    stream has come so far either."""
+    if stream is None or device.type == "cpu":
+        return torch.empty(shape, dtype=dtype, device=device)
+    here = torch.cuda.current_stream(device)
+    if _stream_ptr(stream) == here.cuda_stream:
+        return torch.empty(shape, dtype=dtype, device=device)
+    if not hasattr(stream, "cuda_stream"):
+        stream = torch.cuda.ExternalStream(int(stream), device=device) if int(stream) else torch.cuda.default_stream(device)
+    with torch.cuda.stream(stream):
+        t = torch.empty(shape, dtype=dtype, device=device)
+    t.record_stream(here)
+    return t
+
+
 def _dtype_code(dt: torch.dtype) -> int:
     if dt == torch.float32:
         return FSPAD_F32
@@ -293,13 +311,12 @@ def fspad_tree_attn(q: torch.Tensor, k_tree: torch.Tensor, v_tree: torch.Tensor,
     if kv_len.shape != (desc.batch,) or n_nodes.shape != (desc.batch,):
         raise ValueError("kv_len and n_nodes must have one entry per sequence")
     if out is None:
-        out = torch.empty(q.shape, dtype=torch.float32 if desc.out_dtype == FSPAD_F32 else torch.bfloat16,
-                          device=q.device)
+        out = _empty(stream, q.shape, torch.float32 if desc.out_dtype == FSPAD_F32 else torch.bfloat16, q.device)
     if anc_mask.dtype not in (torch.int64, torch.uint64) or not anc_mask.is_contiguous():
         raise ValueError("anc_mask must be a contiguous 64-bit integer tensor")
     if workspace is None:
         need = fspad_tree_attn_workspace_bytes(desc, int(kv_len.max(initial=0)))
-        workspace = torch.empty(max(need, 16), dtype=torch.uint8, device=q.device)
+        workspace = _empty(stream, max(need, 16), torch.uint8, q.device)
     args = (ctypes.byref(desc), _dev_ptr(q, "q"), _dev_ptr(k_tree, "k_tree"), _dev_ptr(v_tree, "v_tree"),
             _dev_ptr(k_cache, "k_cache"), _dev_ptr(v_cache, "v_cache"),
             kv_len.ctypes.data, n_nodes.ctypes.data, _dev_ptr(anc_mask, "anc_mask"), _dev_ptr(out, "out"),
@@ -312,19 +329,19 @@ def fspad_tree_accept_workspace_bytes(B: int, Nmax: int, V: int) -> int:
     return int(_lib().fspad_tree_accept_workspace_bytes(B, Nmax, V))
 
 
-def _accept_outputs(B, Nmax, device, outputs):
+def _accept_outputs(B, Nmax, device, outputs, stream):
     if outputs is not None:
         return outputs
-    return (torch.empty((B, Nmax), dtype=torch.int32, device=device), torch.empty((B,), dtype=torch.int32, device=device),
-            torch.empty((B, Nmax), dtype=torch.int32, device=device), torch.empty((B,), dtype=torch.int32, device=device))
+    return (_empty(stream, (B, Nmax), torch.int32, device), _empty(stream, (B,), torch.int32, device),
+            _empty(stream, (B, Nmax), torch.int32, device), _empty(stream, (B,), torch.int32, device))
 
 
-def _accept_common(logits, draft_tokens, parent, n_nodes, workspace):
+def _accept_common(logits, draft_tokens, parent, n_nodes, workspace, stream):
     if logits.dim() != 3 or logits.stride(2) != 1 or logits.stride(0) != logits.shape[1] * logits.stride(1):
         raise ValueError("logits must be [B,Nmax,V] with a uniform row stride")
     B, Nmax, V = logits.shape
     if workspace is None:
-        workspace = torch.empty(fspad_tree_accept_workspace_bytes(B, Nmax, V), dtype=torch.uint8, device=logits.device)
+        workspace = _empty(stream, fspad_tree_accept_workspace_bytes(B, Nmax, V), torch.uint8, logits.device)
     for name, t in (("draft_tokens", draft_tokens), ("parent", parent), ("n_nodes", n_nodes)):
         if t.dtype != torch.int32 or not t.is_contiguous():
             raise ValueError(f"{name} must be a contiguous int32 device tensor")
@@ -336,8 +353,8 @@ def fspad_tree_accept_greedy(logits: torch.Tensor, draft_tokens: torch.Tensor, p
                              stream=None, prepare: bool = False):
     """All tensors on the device. Returns (path [B,Nmax], path_len [B], tokens [B,Nmax], n_tokens [B]);
     with prepare=True a PreparedCall."""
-    B, Nmax, V, workspace = _accept_common(logits, draft_tokens, parent, n_nodes, workspace)
-    path, path_len, tokens, n_tokens = _accept_outputs(B, Nmax, logits.device, outputs)
+    B, Nmax, V, workspace = _accept_common(logits, draft_tokens, parent, n_nodes, workspace, stream)
+    path, path_len, tokens, n_tokens = _accept_outputs(B, Nmax, logits.device, outputs, stream)
     args = (B, Nmax, V, _dev_ptr(logits, "logits", torch.float32), logits.stride(1),
             _dev_ptr(draft_tokens, "draft_tokens"), _dev_ptr(parent, "parent"), _dev_ptr(n_nodes, "n_nodes"),
             _dev_ptr(path, "path"), _dev_ptr(path_len, "path_len"), _dev_ptr(tokens, "tokens"),
@@ -373,10 +390,10 @@ def fspad_tree_accept_sample(logits: torch.Tensor, draft_tokens: torch.Tensor, p
                              workspace: Optional[torch.Tensor] = None, stream=None, prepare: bool = False):
     """uniforms: device fp32 [B,2,Nmax] in [0,1). Returns (path, path_len, tokens, n_tokens); with
     prepare=True a PreparedCall."""
-    B, Nmax, V, workspace = _accept_common(logits, draft_tokens, parent, n_nodes, workspace)
+    B, Nmax, V, workspace = _accept_common(logits, draft_tokens, parent, n_nodes, workspace, stream)
     if uniforms.dtype != torch.float32 or not uniforms.is_contiguous() or tuple(uniforms.shape) != (B, 2, Nmax):
         raise ValueError("uniforms must be a contiguous fp32 [B,2,Nmax] device tensor")
-    path, path_len, tokens, n_tokens = _accept_outputs(B, Nmax, logits.device, outputs)
+    path, path_len, tokens, n_tokens = _accept_outputs(B, Nmax, logits.device, outputs, stream)
     args = (B, Nmax, V, _dev_ptr(logits, "logits", torch.float32), logits.stride(1),
             _dev_ptr(draft_tokens, "draft_tokens"), _dev_ptr(parent, "parent"), _dev_ptr(n_nodes, "n_nodes"),
             float(temperature), _dev_ptr(uniforms, "uniforms"),
@@ -400,14 +417,13 @@ def fspad_tree_accept_sample_draft(logits: torch.Tensor, draft_logits: torch.Ten
     [B,2,Nmax]; everything on the device. Returns (path, path_len, tokens, n_tokens); with prepare=True a
     PreparedCall."""
     if workspace is None:
-        workspace = torch.empty(max(16, fspad_tree_accept_sample_draft_workspace_bytes(*logits.shape)), dtype=torch.uint8,
-                                device=logits.device)
-    B, Nmax, V, workspace = _accept_common(logits, draft_tokens, parent, n_nodes, workspace)
+        workspace = _empty(stream, max(16, fspad_tree_accept_sample_draft_workspace_bytes(*logits.shape)), torch.uint8, logits.device)
+    B, Nmax, V, workspace = _accept_common(logits, draft_tokens, parent, n_nodes, workspace, stream)
     if draft_logits.dtype != torch.float32 or draft_logits.shape != logits.shape or draft_logits.stride() != logits.stride():
         raise ValueError("draft_logits must have the dtype, shape and strides of logits")
     if uniforms.dtype != torch.float32 or not uniforms.is_contiguous() or tuple(uniforms.shape) != (B, 2, Nmax):
         raise ValueError("uniforms must be a contiguous fp32 [B,2,Nmax] device tensor")
-    path, path_len, tokens, n_tokens = _accept_outputs(B, Nmax, logits.device, outputs)
+    path, path_len, tokens, n_tokens = _accept_outputs(B, Nmax, logits.device, outputs, stream)
     args = (B, Nmax, V, _dev_ptr(logits, "logits", torch.float32), _dev_ptr(draft_logits, "draft_logits", torch.float32),
             logits.stride(1), _dev_ptr(draft_tokens, "draft_tokens"), _dev_ptr(parent, "parent"),
             _dev_ptr(n_nodes, "n_nodes"), float(temperature), _dev_ptr(uniforms, "uniforms"), _dev_ptr(path, "path"),
@@ -451,12 +467,11 @@ def fspad_tree_accept_greedy_lm_head(hidden: torch.Tensor, lm_head: torch.Tensor
         if t.dtype != torch.int32 or not t.is_contiguous():
             raise ValueError(f"{name} must be a contiguous int32 device tensor")
     if workspace is None:
-        workspace = torch.empty(max(16, fspad_tree_accept_lm_head_workspace_bytes(B, Nmax, V)), dtype=torch.uint8,
-                                device=hidden.device)
-    path, path_len, tokens, n_tokens = _accept_outputs(B, Nmax, hidden.device, outputs)
+        workspace = _empty(stream, max(16, fspad_tree_accept_lm_head_workspace_bytes(B, Nmax, V)), torch.uint8, hidden.device)
+    path, path_len, tokens, n_tokens = _accept_outputs(B, Nmax, hidden.device, outputs, stream)
     if node_outputs is None:
-        node_outputs = (torch.empty((B, Nmax), dtype=torch.int32, device=hidden.device),
-                        torch.empty((B, Nmax), dtype=torch.float32, device=hidden.device))
+        node_outputs = (_empty(stream, (B, Nmax), torch.int32, hidden.device),
+                        _empty(stream, (B, Nmax), torch.float32, hidden.device))
     node_target, node_top = node_outputs
     args = (B, Nmax, V, Hd, _dev_ptr(hidden, "hidden", torch.bfloat16), _dev_ptr(lm_head, "lm_head", torch.bfloat16),
             2 if packed else 0,
@@ -485,9 +500,8 @@ def fspad_tree_accept_sample_lm_head(hidden: torch.Tensor, lm_head: torch.Tensor
     if uniforms.dtype != torch.float32 or not uniforms.is_contiguous() or tuple(uniforms.shape) != (B, 2, Nmax):
         raise ValueError("uniforms must be a contiguous fp32 [B,2,Nmax] device tensor")
     if workspace is None:
-        workspace = torch.empty(max(16, fspad_tree_accept_lm_head_workspace_bytes(B, Nmax, V)), dtype=torch.uint8,
-                                device=hidden.device)
-    path, path_len, tokens, n_tokens = _accept_outputs(B, Nmax, hidden.device, outputs)
+        workspace = _empty(stream, max(16, fspad_tree_accept_lm_head_workspace_bytes(B, Nmax, V)), torch.uint8, hidden.device)
+    path, path_len, tokens, n_tokens = _accept_outputs(B, Nmax, hidden.device, outputs, stream)
     args = (B, Nmax, V, Hd, _dev_ptr(hidden, "hidden", torch.bfloat16), _dev_ptr(lm_head, "lm_head", torch.bfloat16),
             2 if packed else 0,
             _dev_ptr(draft_tokens, "draft_tokens"), _dev_ptr(parent, "parent"), _dev_ptr(n_nodes, "n_nodes"),
@@ -549,7 +563,7 @@ def fspad_pack_weight(w: torch.Tensor, stream=None) -> torch.Tensor:
     need = fspad_packed_weight_bytes(N, K)
     if need == 0:
         raise FspadError(2, "fspad_pack_weight")
-    out = torch.empty(need // 2, dtype=torch.bfloat16, device=w.device)
+    out = _empty(stream, need // 2, torch.bfloat16, w.device)
     _check(_lib().fspad_pack_weight(N, K, _dev_ptr(w, "w"), _dev_ptr(out, "packed"), _stream_ptr(stream)), "fspad_pack_weight")
     return out.view(N, K) if N % 16 == 0 else out
 
@@ -568,9 +582,9 @@ def fspad_feature_sampler(f: torch.Tensor, e: torch.Tensor, w_up: torch.Tensor, 
         if tuple(t.shape) != shape or not t.is_contiguous():
             raise ValueError(f"{name} must be a contiguous {shape} tensor")
     if out is None:
-        out = torch.empty((rows, Hd), dtype=torch.bfloat16, device=f.device)
+        out = _empty(stream, (rows, Hd), torch.bfloat16, f.device)
     if workspace is None:
-        workspace = torch.empty(max(16, fspad_feature_sampler_workspace_bytes(rows, Hd, I)), dtype=torch.uint8, device=f.device)
+        workspace = _empty(stream, max(16, fspad_feature_sampler_workspace_bytes(rows, Hd, I)), torch.uint8, f.device)
     args = (rows, Hd, I, _dev_ptr(f, "f", torch.bfloat16), _dev_ptr(e, "e", torch.bfloat16),
             _dev_ptr(w_up, "w_up", torch.bfloat16), _dev_ptr(w_gate, "w_gate", torch.bfloat16),
             _dev_ptr(w_down, "w_down", torch.bfloat16), (1 if residual else 0) | (2 if packed else 0),
@@ -635,14 +649,14 @@ def fspad_draft_layer(eta: torch.Tensor, positions: torch.Tensor, weights: dict,
     if kv_len.shape != (B,) or n_nodes.shape != (B,):
         raise ValueError("kv_len and n_nodes must have one entry per sequence")
     if outputs is None:
-        outputs = (torch.empty((B, Nmax, Hd), dtype=torch.bfloat16, device=eta.device),
-                   torch.empty((B, Nmax, Hd), dtype=torch.bfloat16, device=eta.device),
-                   torch.empty((B, Nmax, Hkv, D), dtype=torch.bfloat16, device=eta.device),
-                   torch.empty((B, Nmax, Hkv, D), dtype=torch.bfloat16, device=eta.device))
+        outputs = (_empty(stream, (B, Nmax, Hd), torch.bfloat16, eta.device),
+                   _empty(stream, (B, Nmax, Hd), torch.bfloat16, eta.device),
+                   _empty(stream, (B, Nmax, Hkv, D), torch.bfloat16, eta.device),
+                   _empty(stream, (B, Nmax, Hkv, D), torch.bfloat16, eta.device))
     f_tilde, f, k_tree, v_tree = outputs
     if workspace is None:
         need = fspad_draft_layer_workspace_bytes(desc, int(kv_len.max(initial=0)))
-        workspace = torch.empty(max(need, 16), dtype=torch.uint8, device=eta.device)
+        workspace = _empty(stream, max(need, 16), torch.uint8, eta.device)
     args = (ctypes.byref(desc), ctypes.byref(w), _dev_ptr(eta, "eta", torch.bfloat16),
             _dev_ptr(positions, "positions", torch.int32), _dev_ptr(k_cache, "k_cache"), _dev_ptr(v_cache, "v_cache"),
             kv_len.ctypes.data, n_nodes.ctypes.data, _dev_ptr(anc_mask, "anc_mask"),
@@ -756,12 +770,12 @@ def _tree_attn_paged(q, k_tree, v_tree, pages, block_table, kv_len, n_nodes, anc
         raise ValueError("anc_mask must be a contiguous 64-bit integer [B,Nmax] device tensor")
     want = torch.float32 if desc.out_dtype == FSPAD_F32 else torch.bfloat16
     if out is None:
-        out = torch.empty(q.shape, dtype=want, device=q.device)
+        out = _empty(stream, q.shape, want, q.device)
     if out.dtype != want or not out.is_contiguous() or out.shape != q.shape:
         raise ValueError(f"out must be a contiguous {want} tensor of q's shape")
     if workspace is None:
         size_of = fspad_tree_attn_paged_byte_workspace_bytes if fp8 else fspad_tree_attn_paged_workspace_bytes
-        workspace = torch.empty(max(16, size_of(desc)), dtype=torch.uint8, device=q.device)
+        workspace = _empty(stream, max(16, size_of(desc)), torch.uint8, q.device)
     args = (ctypes.byref(desc), _dev_ptr(q, "q"), _dev_ptr(k_tree, "k_tree"), _dev_ptr(v_tree, "v_tree"), _dev_ptr(pages, "pages"),
             _dev_ptr(block_table, "block_table"), _dev_ptr(kv_len, "kv_len"), _dev_ptr(n_nodes, "n_nodes"),
             _dev_ptr(anc_mask, "anc_mask"), _dev_ptr(out, "out"), _dev_ptr(workspace, "workspace"),
@@ -818,7 +832,7 @@ def fspad_kv_store_paged(k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, 
 def _load_paged(slots, pages, head_dim, outputs, stream, prepare, fp8):
     desc = _pool_desc(pages, head_dim, fp8)
     if outputs is None:
-        outputs = tuple(torch.empty((slots.numel(), pages.shape[1], head_dim), dtype=torch.bfloat16, device=pages.device) for _ in range(2))
+        outputs = tuple(_empty(stream, (slots.numel(), pages.shape[1], head_dim), torch.bfloat16, pages.device) for _ in range(2))
     k, v = outputs
     rows, Hkv, D, (row_stride, head_stride) = _paged_rows(k, v, slots)
     if Hkv != pages.shape[1] or D != head_dim:
@@ -854,7 +868,7 @@ def fspad_page_map(kv_len: torch.Tensor, n_new: torch.Tensor, block_table: torch
     if block_table.dtype != torch.int32 or block_table.dim() != 2 or block_table.shape[0] != B or block_table.stride(1) != 1:
         raise ValueError("block_table must be an int32 [B, width] device tensor with contiguous rows")
     if outputs is None:
-        outputs = tuple(torch.empty(shape, dtype=torch.int32, device=kv_len.device)
+        outputs = tuple(_empty(stream, shape, torch.int32, kv_len.device)
                         for shape in ((B, max_new) if max_new is not None else (n_slots,), (B,), (1,), (B,)))
     slots, kv_len_out, n_free_out, granted = outputs
     shapes += [("slots", slots, (B, max_new) if max_new is not None else (n_slots,)), ("kv_len_out", kv_len_out, (B,)),
@@ -906,7 +920,7 @@ def fspad_kv_store_paged_byte(k: torch.Tensor, v: torch.Tensor, slots: torch.Ten
     if pages.shape[1] != Hkv:
         raise ValueError("pages must have the kv heads of k and v")
     if workspace is None:
-        workspace = torch.empty(max(16, fspad_kv_store_paged_byte_workspace_bytes(desc, rows)), dtype=torch.uint8, device=pages.device)
+        workspace = _empty(stream, max(16, fspad_kv_store_paged_byte_workspace_bytes(desc, rows)), torch.uint8, pages.device)
     args = (ctypes.byref(desc), rows, _dev_ptr(k, "k"), _dev_ptr(v, "v"), row_stride, head_stride, _dev_ptr(slots, "slots"),
             _dev_ptr(pages, "pages"), _dev_ptr(workspace, "workspace"), workspace.numel() * workspace.element_size(), _stream_ptr(stream))
     _on_current_device(k, v, slots, pages, workspace)
@@ -935,8 +949,8 @@ def _row_stride(table: torch.Tensor) -> int:
     return table.stride(0) if table.shape[0] > 1 else table.shape[1]   # (of one row the stride says nothing)
 
 
-def _empty_i32(device, *shapes):
-    return tuple(torch.empty(shape, dtype=torch.int32, device=device) for shape in shapes)
+def _empty_i32(stream, device, *shapes):
+    return tuple(_empty(stream, shape, torch.int32, device) for shape in shapes)
 
 
 def fspad_page_fork(src: torch.Tensor, dst: torch.Tensor, kv_len: torch.Tensor, block_table: torch.Tensor, free_pages: torch.Tensor,
@@ -949,7 +963,7 @@ def fspad_page_fork(src: torch.Tensor, dst: torch.Tensor, kv_len: torch.Tensor, 
     B, F, n_pages = kv_len.numel(), src.numel(), free_pages.numel()
     _check_table(block_table, B)
     if outputs is None:
-        outputs = _empty_i32(kv_len.device, (F,), (F,), (B,), (1,), (n_pages,), (F,))
+        outputs = _empty_i32(stream, kv_len.device, (F,), (F,), (B,), (1,), (n_pages,), (F,))
     copy_src, copy_dst, kv_len_out, n_free_out, shared_out, granted = outputs
     _check_i32([("src", src, (F,)), ("dst", dst, (F,)), ("kv_len", kv_len, (B,)), ("free_pages", free_pages, (n_pages,)), ("n_free", n_free, (1,)),
                 ("shared", shared, (n_pages,)), ("copy_src", copy_src, (F,)), ("copy_dst", copy_dst, (F,)), ("kv_len_out", kv_len_out, (B,)),
@@ -976,12 +990,12 @@ def fspad_page_release(ended: torch.Tensor, kv_len: torch.Tensor, block_table: t
     B, n_pages = kv_len.numel(), free_pages.numel()
     _check_table(block_table, B)
     if outputs is None:
-        outputs = _empty_i32(kv_len.device, (B,), (1,), (n_pages,))
+        outputs = _empty_i32(stream, kv_len.device, (B,), (1,), (n_pages,))
     kv_len_out, n_free_out, shared_out = outputs
     _check_i32([("ended", ended, (B,)), ("kv_len", kv_len, (B,)), ("free_pages", free_pages, (n_pages,)), ("n_free", n_free, (1,)), ("shared", shared, (n_pages,)),
                 ("kv_len_out", kv_len_out, (B,)), ("n_free_out", n_free_out, (1,)), ("shared_out", shared_out, (n_pages,))])
     if workspace is None:
-        workspace = torch.empty(max(16, fspad_page_release_workspace_bytes(B, n_pages, block_table.shape[1])), dtype=torch.uint8, device=kv_len.device)
+        workspace = _empty(stream, max(16, fspad_page_release_workspace_bytes(B, n_pages, block_table.shape[1])), torch.uint8, kv_len.device)
     args = (B, int(page_tokens), n_pages, block_table.shape[1], _row_stride(block_table), _dev_ptr(ended, "ended"), _dev_ptr(kv_len, "kv_len"),
             _dev_ptr(block_table, "block_table"), _dev_ptr(free_pages, "free_pages"), _dev_ptr(n_free, "n_free"), _dev_ptr(shared, "shared"),
             *(_dev_ptr(t, "outputs") for t in outputs), _dev_ptr(workspace, "workspace"), workspace.numel() * workspace.element_size(), _stream_ptr(stream))
@@ -998,7 +1012,7 @@ def fspad_page_compact(kv_len: torch.Tensor, block_table: torch.Tensor, free_pag
     B, n_pages = kv_len.numel(), free_pages.numel()
     _check_table(block_table, B)
     if outputs is None:
-        outputs = _empty_i32(kv_len.device, (n_pages // 2,), (n_pages // 2,), tuple(block_table.shape), (n_pages,), (n_pages,))
+        outputs = _empty_i32(stream, kv_len.device, (n_pages // 2,), (n_pages // 2,), tuple(block_table.shape), (n_pages,), (n_pages,))
     copy_src, copy_dst, table_out, free_out, shared_out = outputs
     _check_table(table_out, B, "block_table_out")
     if table_out.shape != block_table.shape:
@@ -1041,11 +1055,10 @@ def fspad_draft_topk(logits: torch.Tensor, k: int, outputs=None, workspace: Opti
         raise ValueError("logits must be [rows,V] with contiguous entries")
     rows, V = logits.shape
     if workspace is None:
-        workspace = torch.empty(max(16, fspad_draft_topk_workspace_bytes(rows, V, k)), dtype=torch.uint8,
-                                device=logits.device)
+        workspace = _empty(stream, max(16, fspad_draft_topk_workspace_bytes(rows, V, k)), torch.uint8, logits.device)
     if outputs is None:
-        outputs = (torch.empty((rows, k), dtype=torch.int32, device=logits.device),
-                   torch.empty((rows, k), dtype=torch.float32, device=logits.device))
+        outputs = (_empty(stream, (rows, k), torch.int32, logits.device),
+                   _empty(stream, (rows, k), torch.float32, logits.device))
     tokens, logp = outputs
     args = (rows, V, int(k), _dev_ptr(logits, "logits", torch.float32), logits.stride(0),
             _dev_ptr(tokens, "tokens", torch.int32), _dev_ptr(logp, "logp", torch.float32),
@@ -1068,9 +1081,9 @@ def fspad_tree_build(cand_parent: torch.Tensor, cand_token: torch.Tensor, cand_l
         raise ValueError("n_cand must be an int32 [B] device tensor")
     dev = cand_parent.device
     if outputs is None:
-        outputs = (torch.empty((B, n_max), dtype=torch.int32, device=dev), torch.empty((B, n_max), dtype=torch.int32, device=dev),
-                   torch.empty((B,), dtype=torch.int32, device=dev), torch.empty((B, n_max), dtype=torch.int64, device=dev),
-                   torch.empty((B, n_max), dtype=torch.int32, device=dev))
+        outputs = (_empty(stream, (B, n_max), torch.int32, dev), _empty(stream, (B, n_max), torch.int32, dev),
+                   _empty(stream, (B,), torch.int32, dev), _empty(stream, (B, n_max), torch.int64, dev),
+                   _empty(stream, (B, n_max), torch.int32, dev))
     parent, tokens, n_nodes, mask, node_cand = outputs
     for name, t, shape in (("parent", parent, (B, n_max)), ("draft_tokens", tokens, (B, n_max)), ("n_nodes", n_nodes, (B,)),
                            ("anc_mask", mask, (B, n_max)), ("node_cand", node_cand, (B, n_max))):

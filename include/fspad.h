@@ -499,6 +499,7 @@ fspad_status fspad_kv_load_paged(const fspad_paged_desc* desc, int32_t rows, con
  * give the same bits from run to run; a sequence's results may differ in their last bits with the batch it is in, which decides how
  * its keys are cut.
  */
+/* How a call is dealt out decides its size, which a smaller batch or bound may well raise: a buffer for several descriptors has the largest of their sizes. */
 size_t fspad_tree_attn_paged_workspace_bytes(const fspad_paged_desc* desc);
 
 fspad_status fspad_tree_attn_paged(const fspad_paged_desc* desc,
@@ -509,8 +510,8 @@ fspad_status fspad_tree_attn_paged(const fspad_paged_desc* desc,
                                    void* workspace, size_t workspace_bytes, void* hip_stream);
 
 /*
- * Paged 8-bit cache (no passage of the paper: a storage format between the bf16 cache, of which it takes half, and the 4-bit one, with errors of
- * 1/16 of a value at most). Block tables, slots, lengths and the stack of free pages are those of the 4-bit cache: fspad_page_map keeps
+ * Paged 8-bit cache (no passage of the paper: a storage format between the bf16 cache, of which it takes half, and the 4-bit one; values are off by
+ * 1/16 at most where they are not small beside the largest of their block). Block tables, slots, lengths and the stack of free pages are those of the 4-bit cache: fspad_page_map keeps
  * them, and descriptors are the same (page_tokens: 32, 64, 128 or 256).
  *
  * Values. A block is 32 neighbouring tokens of a page (from a multiple of 32 on) and one kv head; K and V have scales of their own. An element is
@@ -522,8 +523,10 @@ fspad_status fspad_tree_attn_paged(const fspad_paged_desc* desc,
  *          is not specified then). Else the larger of t and the s that the block has; where it grows, the tokens that the block held are
  *          rounded again, value / 2^(s-127), as below
  *   code = the element nearest to x / 2^(s-127), ties to the even one, at most 448; NaN and infinity become NaN
- * so that a value up to 7 * 2^125 is off by at most 1/16 of it, or by 2^(s-137) where that is more. A scale grows by powers of two: rounding again changes
- * only values that come to lie below 2^-6 of the new one, and those by the same 2^(s-137) at most. What reads a cache takes s from 10 to
+ * so that a value up to 7 * 2^125 is off by at most 1/16 of it from 2^(s-133) on, and by at most 2^(s-137) below that, when it is stored (what is below 2^-19 of
+ * its block's largest becomes 0). A scale grows by powers of two: rounding again changes only values that come to lie below 2^(s-133) of
+ * the new s, and those by 2^(s-137) at most. All growths' errors add up to less than twice the last one's: a value that a block holds under s is
+ * off by less than 1/16 of what was stored plus 2^(s-136), however often the scale has grown. What reads a cache takes s from 10 to
  * 246; other scales are not specified.
  *
  * Pages. A page holds page_tokens tokens of all kv heads of one layer, one head after the other, of each (P = page_tokens, D = head_dim,
@@ -561,7 +564,11 @@ fspad_status fspad_kv_load_paged_byte(const fspad_paged_desc* desc, int32_t rows
 /*
  * fspad_tree_attn_paged over 8-bit pages: arguments, masks, lengths, outputs, workspace and errors are those of that call. Products with cached
  * keys and values, and the roundings of queries, weights and sums, are those that stand there too (cached values are exact in bf16).
+ * max_kv_len decides more here: also how rows are dealt out, so that batches of short sequences take longer under a bound far above them. 256 single tokens of
+ * 100 tokens, 32 heads on 8, 17.9 us under their own length and 40.4 under 8192; 64 trees of 60 nodes, 500 tokens, 61 and 67; 2000 tokens, 168 and 174; one
+ * token, 511 tokens, 8.6 and 11.1; 4 trees on 52 heads, 4096 tokens, 45 either way.
  */
+/* As fspad_tree_attn_paged_workspace_bytes: a smaller batch or bound may take more (60 nodes on 32 heads, 8 of keys, D = 128, under 2500: 64 sequences 8 KB, 11 29 MB, 4 2 KB). */
 size_t fspad_tree_attn_paged_byte_workspace_bytes(const fspad_paged_desc* desc);
 
 fspad_status fspad_tree_attn_paged_byte(const fspad_paged_desc* desc,
@@ -581,9 +588,11 @@ fspad_status fspad_tree_attn_paged_byte(const fspad_paged_desc* desc,
  *   B           rows of the block table, 1..2048;  page_tokens 16, 32, 64, 128 or 256;  n_pages 1..2^19 (n_pages and table_width times page_tokens <= 2^31 - 1)
  *   block_table dev [B] rows of table_width i32, table_stride entries apart (B * table_width <= 2^30)
  *   kv_len      dev [B] i32 (negative lengths count as 0); sequence b holds the first ceil(kv_len[b] / P) entries of its row
- *   free_pages  dev [n_pages] i32, n_free dev [1] i32 (taken as 0..n_pages): the stack of fspad_page_map. It names no page twice and none that is held
+ *   free_pages  dev [n_pages] i32, n_free dev [1] i32 (taken as 0..n_pages): the stack of fspad_page_map. Its first n_free entries are pages, none twice and
+ *               none that is held (others would not be read or written past, but a fork would be granted without its page, and a compaction
+ *               would leave a held page among those that it calls free); what lies behind them is not looked at
  *   outputs     kv_len_out may be kv_len, n_free_out n_free, shared_out shared; else they do not overlap with inputs
- * Entries of tables and of the stack outside [0,n_pages) count for no page. None of the calls allocates or synchronises; results are the same from run to run.
+ * Entries of tables outside [0,n_pages) count for no page. None of the calls allocates or synchronises; results are the same from run to run.
  */
 
 /*

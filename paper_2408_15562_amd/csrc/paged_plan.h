@@ -23,7 +23,7 @@ constexpr int kSlabWhole = 96;   // units of so many blocks are not cut where a 
 
 struct PagedPlan {
   int rows_per_wave, WS, waves;   // row slabs and wavefronts of a workgroup (those of a slab split its keys)
-  int rows_per_group;    // WS * rows_per_wave: 16, 32 or 64
+  int rows_per_group;    // WS * rows_per_wave: 16, 32, 64 or 128
   int groups;            // row groups of a kv head's N * G rows
   int resident;          // workgroups that the device holds at once
   int least_blocks, whole_blocks;   // no piece is shorter, no unit of up to so many blocks is cut
@@ -39,18 +39,23 @@ inline int64_t paged_unit_blocks(const fspad_paged_desc& d) {   // at most
   return ((int64_t)d.max_kv_len + kBlockKeys - 1) / kBlockKeys + (d.n_nodes_max + kBlockKeys - 1) / kBlockKeys;
 }
 
-// How a call over the 8-bit cache deals its rows out: in slabs of 16 or 32 rows (WS of them a workgroup), and a slab's keys to `key_waves` wavefronts. Two slabs, or one of 64 rows,
-// in a workgroup read keys once for both, but a workgroup of one slab is lighter, and a wavefront that has all keys of its rows merges nothing. Chosen / otherwise, us; query heads on kv heads:
-// Fewer slabs than compute units: one a workgroup, four wavefronts up to 72 blocks, then eight, if the pieces fill three quarters of the device. 60 nodes, 16 on 16, D = 128, in groups of 64 rows: 4 sequences of 300
-//   tokens 11.2 / 14.0, 1000 15.0 / 19.7, 2000 18.4 / 23.9, on eight wavefronts 19.1; 32 on 8: 4 of 1000 15.7 / 20.3, 2000 19.8 / 29.4, 4000 26 / 33, on four 32; 64 on 8, 16384 44 / 46. D = 64: 4 of 1000 11.7 / 16.3,
-//   4000 18 / 23. 160 rows of 32 heads, 9946 tokens: 48 / 57 in slabs.
-// More: the same on four wavefronts up to 72 blocks; D = 128 from 37 on. 4 of 60 nodes, 64 on 8: 500 tokens 17.4 / 18.4 in slabs, 2000 28 / 31; D = 64: 500 13.1 / 14.6, 2000 21 / 24; 4 of 36 on 40, 8000 49 / 64 in slabs.
-// Three a compute unit (16 rows: four; long ones, D = 64: six) and more than 64 rows: four a workgroup, a wavefront each. 60 nodes, 32 on 8, D = 128: 8 sequences (512 slabs) of 500 17.4 / 20.6 so, 12 (768)
-//   21.5 / 24, of 2000 41 / 59, of 50 .. 4000 64 / 70, 64 of 500 70 / 91, of 2000 168 / 249. D = 64: 12 of 2000 31 / 35, of 8000 80 / 83 so, 64 of 500 40 / 70.
-// The same, 64 rows or fewer, up to 72 blocks: a workgroup is a slab, of one wavefront where they are short or six a compute unit, else of two. One token, 32 on 8, D = 128: 64 sequences (512 slabs) of 250
-//   12.0 / 12.5 so, 128 (1024) of 30 9.3 / 13.8, of 500 30 / 36 on four and on one, of 50 .. 2000 62 / 69 and 69, of 4000 182 / 193 so; 256 of 100 19 / 36 on four, of 1000 100 / 104. D = 64: 128 of 50 .. 2000 35 / 39 and 43. 7 nodes,
-//   D = 128: 64 of 50 .. 1000 22 / 25 so, 96 (768) of 500 27 / 31 and 30, 256 of 500 64 / 81; D = 64: 96 of 50 .. 2000 32 / 40 and 41. 60 nodes, 16 on 16: 32 (1024) of 1000 39 / 45 and 44, of 1000 .. 8000 172 / 228 so.
-// More than 32 rows and few keys: one wavefront a slab. 60 nodes, 32 on 8, D = 128: one token 10.2 / 11.4, 250 13.2 / 13.2; D = 64: 8.6 / 9.4, 250 11.0 / 12.0, 500 13.5 / 13.5.
+// How a call over the 8-bit cache deals its rows out: in slabs of 16 or 32 rows (WS of them a workgroup), and a slab's keys to `key_waves` wavefronts.
+// Two slabs, or one of 64 rows, in a workgroup read keys once for both (the 4-bit cache's way); a workgroup of one slab is lighter, and a wavefront that
+// has all keys of its rows merges nothing. Below, us: by the rule / the 4-bit way, or slabs x wavefronts of a slab; D = 128 where nothing is said,
+// query heads on kv heads. profiles/paged_fp8_dealing.txt has every way for 48 calls, and 200 drawn calls by the rule and the 4-bit way.
+//  - No more slabs than compute units: one a workgroup, four wavefronts up to 72 blocks, then eight if the pieces fill three quarters of the device.
+//    4 x 60 nodes, 16 on 16: 300 tokens 10.5 / 13.1, 1 x 8 12.3; 2000 17.3 / 22.4, 1 x 8 18.0. 32 on 8: 2000 17.5 / 26.8; 4000 25.7 / 31.7, 1 x 4 31.6.
+//    D = 64: 1000 10.6 / 15.2, 1 x 8 11.0; 4000 17.1 / 25.3, 1 x 4 22.8. 1 x 60 nodes, 64 on 8, 16384: 44.0 / 44.9
+//  - More: the same on four wavefronts up to 72 blocks, D = 128 from 37 on. 4 x 60 nodes, 64 on 8: 2000 26.0 / 28.6; D = 64 500 12.0 / 13.4, 2000 18.3 / 20.7;
+//    as the 4-bit cache: 500 15.3, 1 x 4 16.1; 36 nodes, 40 on 40, 8000 82, 1 x 4 111, 1 x 2 76
+//  - Three a compute unit (16 rows: four; long ones, D = 64: six) and more than 64 rows: four a workgroup, a wavefront each. 60 nodes, 32 on 8: 12 sequences of
+//    50 .. 4000 53 / 58, 1 x 4 60; 64 of 500 64 / 83, 1 x 4 110; 64 of 2000 166 / 245. D = 64: 64 of 500 38 / 66, 1 x 4 78. It loses a little where a unit is long
+//    and the device has no more than two rounds of them: D = 64, 12 of 2000 30.0 / 31.9, 1 x 4 25.3; 101 of 39 nodes, 48 on 12, 7250 769 / 665
+//  - The same, 64 rows or fewer, up to 72 blocks: a slab a workgroup, one wavefront where they are short or six a compute unit, else two. One token, 32 on 8:
+//    128 of 30 8.1 / 11.9, 256 of 100 17.8 / 34.1, 1 x 2 23.4, 128 of 500 25.0 / 28.0, 1 x 1 26.8. 7 nodes: 96 of 500 24.1 / 26.8, 1 x 1 23.7, 256 of 500 53 / 70, 1 x 2 58;
+//    D = 64, 96 of 50 .. 2000 27.7 / 34.9, 1 x 1 30.2. 60 nodes, 16 on 16: 32 of 1000 31.7 / 40.6
+//  - More than 32 rows and few keys: one wavefront a slab. 60 nodes, 32 on 8: one token 9.8 / 11.0, 150 11.5 / 12.3; D = 64: 8.1 / 9.0, 250 10.6 / 11.5 (1 x 4, which was
+//    measured after the rule was made: 8.4, 9.8, 6.7, 8.4)
 struct PagedRows {
   int per_wave, WS, key_waves;   // key_waves 0: as over the 4-bit cache
 };

@@ -544,7 +544,7 @@ size_t fspad_kv_page_bytes_byte(int32_t n_kv_heads, int32_t head_dim, int32_t pa
 /*
  * Keys and values of `rows` tokens into the slots they are given, as fspad_kv_store_paged, rounded as above.
  *   k, v, slots, row_stride, head_stride   as there. The rows of a block may stand anywhere in the call. No slot may be given to two rows of a
- *             call (what the block holds of it then is not specified)
+ *             call (what its block holds then, of its other tokens too, is not specified)
  *   rows      0..1048560; 0 does nothing (no pointer is looked at)
  *   pages     dev, 16-byte aligned. Tokens of other blocks stay as they are; no other call may use a block that this one stores to meanwhile
  *   workspace dev, 16-byte aligned, >= fspad_kv_store_paged_byte_workspace_bytes(desc, rows): 0 up to 2048 rows (may be NULL then), 4 bytes a
